@@ -388,6 +388,62 @@ int polestar_k_confidence(const float *logits_dev, int32_t rows, int32_t vocab, 
 int polestar_k_confidence_noalloc(const float *logits_dev, int32_t rows, int32_t vocab, int32_t mask_id,
                                   int32_t *yhat_dev, float *conf_dev, void *cuda_stream);
 
+/* ---- microscaled 4-bit floating point: rows, products, a K/V cache ------------------------- */
+/* The hidden cache's NVFP4 format without a reference row, and the OCP MX format beside it (the paper quantises hidden states
+ * only, Appendix "Quantization Format"; weights and keys / values in the same format are this library's).
+ * A row of d channels is d/2 bytes of E2M1 codes (channel 2i in the low nibble: bit 3 sign, bits 0-2 index into {0, .5, 1, 1.5, 2, 3,
+ * 4, 6}) and a scale byte per group of channels.  With t the tensor's factor (one positive normal float on the device; a null
+ * pointer stands for 1), float32 arithmetic with IEEE division:
+ *   POLESTAR_FP4_NV  16 channels, s = E4M3(amax / (6 t)), nearest even, saturating at 448
+ *   POLESTAR_FP4_MX  32 channels, s = 2^clamp(floor(log2(amax / t)) - 2, -127, 127), byte = exponent + 127 (E8M0)
+ *   code = grid value nearest to |x| / (s t), ties to the even code, saturating at 6;  stored value = code * s * t
+ * A group with an infinity or NaN has the scale NaN (0x7f / 0xff) and zero codes; a group whose scale rounds to zero is zero.
+ * Scale bytes lie
+ *   POLESTAR_SCALES_ROWS   row-major [rows][d / 16 or 32], or
+ *   POLESTAR_SCALES_TILED  as the product reads them: blocks of 512 bytes for 128 rows x 4 groups, block (r / 128, g / 4) row-major,
+ *                          byte (r % 32) * 16 + (r % 128 / 32) * 4 + g % 4; rows and groups that do not exist are zero bytes. */
+#define POLESTAR_FP4_NV 0
+#define POLESTAR_FP4_MX 1
+#define POLESTAR_SCALES_ROWS  0
+#define POLESTAR_SCALES_TILED 1
+
+/* Bytes of the scales of [rows][d] (0: bad arguments, or no rows). */
+size_t polestar_k_fp4_scale_bytes(int64_t rows, int32_t d, int32_t format, int32_t layout);
+
+/* Quantise rows.  x_dev [rows][d], row stride ld_x elements (>= d, a multiple of 16 bytes), dtype POLESTAR_F32 or _BF16, 16-byte
+ * aligned; d % 32 == 0; codes_dev uint8 [rows][d/2], 4-byte aligned; scales_dev as above (TILED: 4-byte aligned);
+ * deq_dev [rows][d] the stored values in x's type (rounded once; NULL: skipped), 16-byte aligned. */
+int polestar_k_fp4_quantize(const void *x_dev, int64_t ld_x, int32_t rows, int32_t d, int32_t dtype, int32_t format,
+                            int32_t scale_layout, const float *tensor_scale_dev, uint8_t *codes_dev, uint8_t *scales_dev,
+                            void *deq_dev, void *cuda_stream);
+
+/* Rows of keys and values into a cache held in 4 bits (format NV, scales row-major):
+ *   k_dev / v_dev [batch][R][n_kv*head_dim], F32 or BF16, 16-byte aligned; head_dim 64 or 128
+ *   idx_dev int32 [batch][R]: position of every row in its sequence (NULL: row i goes to position i); count_dev int32 [batch]: rows listed
+ *   (NULL: R; clamped to 0 .. R).  A position outside [0, cap) is skipped; of rows that list the same position the last one stays.
+ *   kc_dev / vc_dev uint8 [batch][cap][n_kv][head_dim/2], 4-byte aligned, ks_dev / vs_dev uint8 [batch][cap][n_kv][head_dim/16]
+ *   k_scale_dev / v_scale_dev: the tensor factors t of keys and values (NULL: 1)
+ *   k_deq_dev / v_deq_dev: stored values of the listed rows, shape and type of k_dev (NULL: skipped)
+ * Cache rows and stored values that no listed row belongs to are left as they were.  1 <= cap <= 65536, R <= 65536. */
+int polestar_k_kv4_append(const void *k_dev, const void *v_dev, const int32_t *idx_dev, const int32_t *count_dev, int32_t batch,
+                          int32_t R, int32_t cap, int32_t n_kv, int32_t head_dim, int32_t dtype, const float *k_scale_dev,
+                          const float *v_scale_dev, uint8_t *kc_dev, uint8_t *ks_dev, uint8_t *vc_dev, uint8_t *vs_dev,
+                          void *k_deq_dev, void *v_deq_dev, void *cuda_stream);
+
+/* Log-probability of a given token, entropy and the most likely alternatives of logits rows (the quantities next to the
+ * confidence of Eq. 1 that samplers commit by and servers report; the softmax runs over the full vocabulary).
+ *   logits_dev [rows][vocab], F32 or BF16, row stride ld elements (>= vocab), any alignment of the element's size
+ *   target_dev int32 [rows]: logprob_dev[r] = log softmax(row r)[target[r]]; a negative target gives 0, one >= vocab NaN
+ *   entropy_dev[r] = -sum p log p (natural logarithm)
+ *   top_ids_dev int32 / top_logprobs_dev float [rows][top_k]: the top_k most likely tokens other than mask_id (out of range: none left
+ *   out), most likely first, the lowest id first among equals; -1 / -inf where the vocabulary has fewer
+ * logprob_dev (with target_dev) and entropy_dev may be NULL, and the top pointers with top_k = 0.  A row with NaN or +inf, or with nothing
+ * above -inf, has NaN in all its results (ids in range, never a NaN's).  0 <= top_k <= POLESTAR_LOGPROBS_MAX_TOP. */
+#define POLESTAR_LOGPROBS_MAX_TOP 32
+int polestar_k_token_logprobs(const void *logits_dev, int64_t ld, int32_t rows, int32_t vocab, int32_t dtype,
+                              const int32_t *target_dev, int32_t mask_id, int32_t top_k, float *logprob_dev,
+                              float *entropy_dev, int32_t *top_ids_dev, float *top_logprobs_dev, void *cuda_stream);
+
 /* Number of SMs of the device the library last sized grids for (0 before any call that launches kernels). */
 int polestar_sm_count(void);
 

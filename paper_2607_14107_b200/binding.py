@@ -37,6 +37,7 @@ EXPORTS = [
     "polestar_k_attention", "polestar_k_hidden_delta", "polestar_k_select",
     "polestar_k_refresh_scratch_bytes", "polestar_k_refresh", "polestar_k_confidence",
     "polestar_k_confidence_noalloc", "polestar_sm_count",
+    "polestar_k_fp4_scale_bytes", "polestar_k_fp4_quantize", "polestar_k_kv4_append", "polestar_k_token_logprobs",
 ]
 
 
@@ -139,6 +140,15 @@ def load():
     lib.polestar_reload_env.argtypes = []
     lib.polestar_k_refresh_status.restype = C.c_int
     lib.polestar_k_refresh_status.argtypes = [vp, sz, i32, i32, i32, i32, vp]
+    i64 = C.c_int64
+    lib.polestar_k_fp4_scale_bytes.restype = sz
+    lib.polestar_k_fp4_scale_bytes.argtypes = [i64, i32, i32, i32]
+    lib.polestar_k_fp4_quantize.restype = C.c_int
+    lib.polestar_k_fp4_quantize.argtypes = [vp, i64, i32, i32, i32, i32, i32, vp, vp, vp, vp, vp]
+    lib.polestar_k_kv4_append.restype = C.c_int
+    lib.polestar_k_kv4_append.argtypes = [vp, vp, vp, vp] + [i32] * 6 + [vp] * 9
+    lib.polestar_k_token_logprobs.restype = C.c_int
+    lib.polestar_k_token_logprobs.argtypes = [vp, i64, i32, i32, i32, vp, i32, i32, vp, vp, vp, vp, vp]
     _lib = lib
     return lib
 
@@ -462,3 +472,100 @@ def polestar_k_confidence_noalloc(logits, mask_id, yhat, conf):
     rows, V = logits.shape
     _check(load().polestar_k_confidence_noalloc(_ptr(logits), rows, V, mask_id, _ptr(yhat), _ptr(conf),
                                                 C.c_void_p(_stream())))
+
+
+# ------------------------------------------------------------------------------------------
+# microscaled 4-bit floating point, token log-probabilities
+# ------------------------------------------------------------------------------------------
+
+FP4_NV, FP4_MX = 0, 1
+SCALES_ROWS, SCALES_TILED = 0, 1
+LOGPROBS_MAX_TOP = 32
+
+
+def _need(ok: bool, msg: str) -> None:
+    if not ok:
+        raise PolestarError(E_INVAL, msg)
+
+
+def _buffer(name: str, t: Optional[torch.Tensor], dtype, shape=None, optional: bool = False) -> None:
+    """A dense tensor of this type (and shape) on the current device: the library gets its address only."""
+    if t is None:
+        _need(optional, f"{name} is missing")
+        return
+    _need(t.is_cuda and t.device.index == torch.cuda.current_device(), f"{name} is on {t.device}, not on the current CUDA device")
+    _need(t.dtype == dtype, f"{name} has the type {t.dtype}, not {dtype}")
+    _need(shape is None or tuple(t.shape) == tuple(shape), f"{name} has the shape {tuple(t.shape)}, not {tuple(shape or ())}")
+    _need(t.is_contiguous(), f"{name} is not contiguous")
+
+
+def _row_stride(name: str, t: torch.Tensor) -> int:
+    """Elements between the rows of a matrix whose rows are dense."""
+    _need(t.is_cuda and t.device.index == torch.cuda.current_device(), f"{name} is on {t.device}, not on the current CUDA device")
+    _need(t.dim() == 2, f"{name} has {t.dim()} dimensions, not 2")
+    _need(t.shape[1] <= 1 or t.stride(1) == 1, f"{name} has rows that are not dense")
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+
+def fp4_group(fmt: int) -> int:
+    return 16 if fmt == FP4_NV else 32
+
+
+def polestar_k_fp4_scale_bytes(rows: int, d: int, fmt: int, layout: int) -> int:
+    return int(load().polestar_k_fp4_scale_bytes(rows, d, fmt, layout))
+
+
+def polestar_k_fp4_quantize(x, codes, scales, fmt: int, layout: int = SCALES_ROWS, tensor_scale=None, deq=None):
+    """x [rows][d] (rows may be strided) -> codes uint8 [rows][d/2], scales uint8 of polestar_k_fp4_scale_bytes() bytes, deq like x."""
+    ld = _row_stride("x", x)
+    rows, d = x.shape
+    _buffer("codes", codes, torch.uint8, (rows, d // 2))
+    _buffer("scales", scales, torch.uint8)
+    _need(d % 32 == 0 and scales.numel() == polestar_k_fp4_scale_bytes(rows, d, fmt, layout), "scales have the wrong size for these rows")
+    _buffer("tensor_scale", tensor_scale, torch.float32, (1,), optional=True)
+    _buffer("deq", deq, x.dtype, (rows, d), optional=True)
+    _check(load().polestar_k_fp4_quantize(_ptr(x), ld, rows, d, _dtype_code(x), fmt, layout, _ptr(tensor_scale), _ptr(codes), _ptr(scales),
+                                          _ptr(deq), C.c_void_p(_stream())))
+
+
+def _kv4_cache(kc, ks, vc, vs):
+    """Shape of a 4-bit K/V cache: batch, cap, n_kv, head_dim."""
+    _need(kc.dim() == 4, "kc has to be [batch][cap][n_kv][head_dim/2]")
+    b, cap, n_kv, half = kc.shape
+    for name, t, shape in (("kc", kc, kc.shape), ("vc", vc, kc.shape), ("ks", ks, (b, cap, n_kv, half // 8)), ("vs", vs, (b, cap, n_kv, half // 8))):
+        _buffer(name, t, torch.uint8, shape)
+    return b, cap, n_kv, 2 * half
+
+
+def polestar_k_kv4_append(k, v, idx, counts, kc, ks, vc, vs, k_scale=None, v_scale=None, k_deq=None, v_deq=None):
+    """k, v [batch][R][n_kv*head_dim] into the cache rows idx [batch][R] (None: rows 0 .. R-1), of which counts [batch] are listed (None: R)."""
+    b, cap, n_kv, dh = _kv4_cache(kc, ks, vc, vs)
+    _need(k.dim() == 3, "k has to be [batch][R][n_kv*head_dim]")
+    R = k.shape[1]
+    for name, t in (("k", k), ("v", v)):
+        _buffer(name, t, k.dtype, (b, R, n_kv * dh))
+    for name, t in (("k_deq", k_deq), ("v_deq", v_deq)):
+        _buffer(name, t, k.dtype, k.shape, optional=True)
+    _buffer("idx", idx, torch.int32, (b, R), optional=True)
+    _buffer("counts", counts, torch.int32, (b,), optional=True)
+    for name, t in (("k_scale", k_scale), ("v_scale", v_scale)):
+        _buffer(name, t, torch.float32, (1,), optional=True)
+    _check(load().polestar_k_kv4_append(_ptr(k), _ptr(v), _ptr(idx), _ptr(counts), b, R, cap, n_kv, dh, _dtype_code(k), _ptr(k_scale),
+                                        _ptr(v_scale), _ptr(kc), _ptr(ks), _ptr(vc), _ptr(vs), _ptr(k_deq), _ptr(v_deq),
+                                        C.c_void_p(_stream())))
+
+
+def polestar_k_token_logprobs(logits, target, mask_id, logprob, entropy, top_ids=None, top_logprobs=None):
+    """logits [rows][vocab] (rows may be strided), target int32 [rows] -> logprob, entropy [rows], top_ids / top_logprobs [rows][k]."""
+    ld = _row_stride("logits", logits)
+    rows, V = logits.shape
+    _buffer("target", target, torch.int32, (rows,), optional=logprob is None)
+    _buffer("logprob", logprob, torch.float32, (rows,), optional=True)
+    _buffer("entropy", entropy, torch.float32, (rows,), optional=True)
+    _need((top_ids is None) == (top_logprobs is None), "top_ids and top_logprobs come together")
+    _need(top_ids is None or top_ids.dim() == 2, "top_ids has to be [rows][k]")
+    k = 0 if top_ids is None else top_ids.shape[1]
+    _buffer("top_ids", top_ids, torch.int32, (rows, k), optional=True)
+    _buffer("top_logprobs", top_logprobs, torch.float32, (rows, k), optional=True)
+    _check(load().polestar_k_token_logprobs(_ptr(logits), ld, rows, V, _dtype_code(logits), _ptr(target), -1 if mask_id is None else mask_id, k,
+                                            _ptr(logprob), _ptr(entropy), _ptr(top_ids), _ptr(top_logprobs), C.c_void_p(_stream())))

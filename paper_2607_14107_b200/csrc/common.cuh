@@ -64,7 +64,7 @@ __device__ __forceinline__ uint32_t cluster_rank() {
 // its dependencies are resolved; consecutive stamps give each kernel's real cost inside the pipeline.  The
 // default build compiles none of this.
 #ifdef POLESTAR_TRACE
-__device__ long long* g_trace_buf = nullptr;   // [0] = next slot, then pairs (id, time)
+static __device__ long long* g_trace_buf = nullptr;   // [0] = next slot, then pairs (id, time)
 __device__ __forceinline__ void trace_stamp(int id, int thread = 0) {
     long long* t = g_trace_buf;
     if (t && blockIdx.x == 0 && blockIdx.y == 0 && blockIdx.z == 0 && threadIdx.x == thread) {

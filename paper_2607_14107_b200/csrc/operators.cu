@@ -1,0 +1,152 @@
+// Host side of the operators next to the decoding path: 4-bit rows, products and K/V caches, token log-probabilities.
+// A translation unit of its own, so that it and the path compile side by side.
+#include "../../include/polestar.h"
+
+#include <cuda.h>
+#include <cuda_runtime.h>
+
+#include <algorithm>
+#include <climits>
+#include <mutex>
+
+#include "fp4.cuh"
+#include "logprobs.cuh"
+
+using namespace ps;
+
+#define CK(call) do { if ((call) != cudaSuccess) return POLESTAR_E_CUDA; } while (0)
+
+// Facts of the CURRENT device; the first call on a device queries them and raises the shared-memory limits of the kernels that need
+// more than the default there (function attributes are per device).
+struct DevInfo { bool ready = false; int sm_count = 0; };
+static const int MAX_DEVICES = 64;
+static std::mutex g_mu;
+static DevInfo g_dev[MAX_DEVICES];
+static int device_info(DevInfo* out) {
+    int dev = 0;
+    CK(cudaGetDevice(&dev));
+    if (dev < 0 || dev >= MAX_DEVICES) return POLESTAR_E_INVAL;
+    std::lock_guard<std::mutex> lk(g_mu);
+    DevInfo& di = g_dev[dev];
+    if (!di.ready) {
+        CK(cudaDeviceGetAttribute(&di.sm_count, cudaDevAttrMultiProcessorCount, dev));
+        di.ready = true;
+    }
+    *out = di;
+    return POLESTAR_OK;
+}
+
+// ------------------------------------------------------------------------------------------
+// microscaled 4-bit floating point
+// ------------------------------------------------------------------------------------------
+static bool fp4_format_ok(int format, int layout) {
+    return (format == POLESTAR_FP4_NV || format == POLESTAR_FP4_MX) && (layout == POLESTAR_SCALES_ROWS || layout == POLESTAR_SCALES_TILED);
+}
+
+extern "C" size_t polestar_k_fp4_scale_bytes(int64_t rows, int32_t d, int32_t format, int32_t layout) {
+    if (!fp4_format_ok(format, layout) || rows < 0 || rows > INT32_MAX || d <= 0 || d % 32) return 0;
+    const size_t groups = (size_t)d / fp4::group(format);
+    if (layout == POLESTAR_SCALES_ROWS) return (size_t)rows * groups;
+    return ((size_t)rows + 127) / 128 * ((groups + 3) / 4) * 512;
+}
+
+template <typename T, int FMT>
+static cudaError_t launch_quantize(const fp4::QuantArgs& a, int sms, cudaStream_t st) {
+    // One piece of 16 bytes per thread while that leaves SMs idle (a block of rows is latency), four where the loads have to be many:
+    const long long pieces = a.rows * (a.d / fp4::Vec<T>::N);
+    const bool deep = pieces >= 4LL * fp4::THREADS * 8 * sms;
+    const long long per = fp4::THREADS * (deep ? 4LL : 1LL), blocks = (pieces + per - 1) / per;
+    if (blocks > INT32_MAX) return cudaErrorInvalidValue;
+    if (deep) return launch_k(fp4::quantize_kernel<T, FMT, 4>, dim3((unsigned)blocks), dim3(fp4::THREADS), 0, st, a);
+    return launch_k(fp4::quantize_kernel<T, FMT, 1>, dim3((unsigned)blocks), dim3(fp4::THREADS), 0, st, a);
+}
+
+extern "C" int polestar_k_fp4_quantize(const void* x, int64_t ld_x, int32_t rows, int32_t d, int32_t dtype, int32_t format,
+                                       int32_t scale_layout, const float* tensor_scale, uint8_t* codes, uint8_t* scales, void* deq,
+                                       void* stream) {
+    if (rows < 0 || d <= 0 || d % 32 || !fp4_format_ok(format, scale_layout)) return POLESTAR_E_INVAL;
+    if (dtype != POLESTAR_F32 && dtype != POLESTAR_BF16) return POLESTAR_E_INVAL;
+    const int per16 = dtype == POLESTAR_BF16 ? 8 : 4;
+    if (ld_x < d || ld_x % per16) return POLESTAR_E_INVAL;
+    if (rows == 0) return POLESTAR_OK;           // no rows: nothing to do (the pointers may be null)
+    if (!x || !codes || !scales) return POLESTAR_E_INVAL;
+    if ((((uintptr_t)x | (uintptr_t)deq) & 15) || (((uintptr_t)codes | (uintptr_t)tensor_scale) & 3)) return POLESTAR_E_INVAL;
+    if (scale_layout == POLESTAR_SCALES_TILED && ((uintptr_t)scales & 3)) return POLESTAR_E_INVAL;
+    DevInfo di;
+    int rc = device_info(&di);
+    if (rc) return rc;
+    fp4::QuantArgs a;
+    a.x = x; a.ld_x = ld_x; a.deq = deq; a.ld_deq = d; a.codes = codes; a.scales = scales; a.t = tensor_scale;
+    a.rows = rows; a.d = d; a.layout = scale_layout;
+    cudaStream_t st = (cudaStream_t)stream;
+    const bool nv = format == POLESTAR_FP4_NV;
+    if (dtype == POLESTAR_BF16) CK(nv ? (launch_quantize<__nv_bfloat16, fp4::NV>(a, di.sm_count, st)) : (launch_quantize<__nv_bfloat16, fp4::MX>(a, di.sm_count, st)));
+    else CK(nv ? (launch_quantize<float, fp4::NV>(a, di.sm_count, st)) : (launch_quantize<float, fp4::MX>(a, di.sm_count, st)));
+    return POLESTAR_OK;
+}
+
+// A cache of keys and values in 4 bits: what append and attention accept of its geometry.
+static bool kv4_shape_ok(int batch, int R, int cap, int n_kv, int head_dim) {
+    return batch >= 0 && batch <= 65535 && R >= 0 && cap > 0 && cap <= 65536 && n_kv > 0 && n_kv <= 1024 && (head_dim == 64 || head_dim == 128);
+}
+
+extern "C" int polestar_k_kv4_append(const void* k, const void* v, const int32_t* idx, const int32_t* count, int32_t batch, int32_t R,
+                                     int32_t cap, int32_t n_kv, int32_t head_dim, int32_t dtype, const float* k_scale,
+                                     const float* v_scale, uint8_t* kc, uint8_t* ks, uint8_t* vc, uint8_t* vs, void* k_deq, void* v_deq,
+                                     void* stream) {
+    if (!kv4_shape_ok(batch, R, cap, n_kv, head_dim) || R > 65536) return POLESTAR_E_INVAL;
+    if (dtype != POLESTAR_F32 && dtype != POLESTAR_BF16) return POLESTAR_E_INVAL;
+    if (batch == 0 || R == 0) return POLESTAR_OK;         // no rows: nothing to do (the pointers may be null)
+    if (!k || !v || !kc || !ks || !vc || !vs) return POLESTAR_E_INVAL;
+    if (((uintptr_t)k | (uintptr_t)v | (uintptr_t)k_deq | (uintptr_t)v_deq) & 15) return POLESTAR_E_INVAL;
+    if (((uintptr_t)kc | (uintptr_t)vc | (uintptr_t)idx | (uintptr_t)count | (uintptr_t)k_scale | (uintptr_t)v_scale) & 3) return POLESTAR_E_INVAL;
+    DevInfo di;
+    int rc = device_info(&di);
+    if (rc) return rc;
+    fp4::AppendArgs a;
+    a.x[0] = k; a.x[1] = v; a.deq[0] = k_deq; a.deq[1] = v_deq; a.codes[0] = kc; a.codes[1] = vc; a.scales[0] = ks; a.scales[1] = vs;
+    a.t[0] = k_scale; a.t[1] = v_scale; a.idx = idx; a.counts = count; a.R = R; a.cap = cap; a.width = n_kv * head_dim;
+    // rows of a block: four rounds of loads' worth, so that a long list is not scanned by every row, while there are blocks for all SMs
+    const int pieces = a.width / (dtype == POLESTAR_BF16 ? 8 : 4);
+    int rpb = std::max(1, fp4::THREADS / pieces);
+    while (rpb * 2 <= fp4::APPEND_MAX_ROWS && rpb * pieces < 8 * fp4::THREADS && 2LL * batch * ((R + 2 * rpb - 1) / (2 * rpb)) >= 8LL * di.sm_count) rpb *= 2;
+    a.rows_per_block = std::min(rpb, fp4::APPEND_MAX_ROWS);
+    const dim3 grid((R + a.rows_per_block - 1) / a.rows_per_block, batch, 2);
+    if (dtype == POLESTAR_BF16) CK(launch_k(fp4::kv_append_kernel<__nv_bfloat16>, grid, dim3(fp4::THREADS), 0, (cudaStream_t)stream, a));
+    else CK(launch_k(fp4::kv_append_kernel<float>, grid, dim3(fp4::THREADS), 0, (cudaStream_t)stream, a));
+    return POLESTAR_OK;
+}
+
+// ------------------------------------------------------------------------------------------
+// token log-probabilities
+// ------------------------------------------------------------------------------------------
+extern "C" int polestar_k_token_logprobs(const void* logits, int64_t ld, int32_t rows, int32_t vocab, int32_t dtype,
+                                         const int32_t* target, int32_t mask_id, int32_t top_k, float* logprob, float* entropy,
+                                         int32_t* top_ids, float* top_logprobs, void* stream) {
+    if (rows < 0 || vocab <= 0 || top_k < 0 || top_k > POLESTAR_LOGPROBS_MAX_TOP || ld < vocab) return POLESTAR_E_INVAL;
+    if (dtype != POLESTAR_F32 && dtype != POLESTAR_BF16) return POLESTAR_E_INVAL;
+    if (rows == 0) return POLESTAR_OK;           // no rows: nothing to do (the pointers may be null)
+    if (!logits || (logprob && !target) || (top_k > 0 && (!top_ids || !top_logprobs))) return POLESTAR_E_INVAL;
+    const int es = dtype == POLESTAR_BF16 ? 2 : 4;
+    if (((uintptr_t)logits & (es - 1)) || (((uintptr_t)target | (uintptr_t)logprob | (uintptr_t)entropy | (uintptr_t)top_ids | (uintptr_t)top_logprobs) & 3))
+        return POLESTAR_E_INVAL;
+    DevInfo di;
+    int rc = device_info(&di);
+    if (rc) return rc;
+    lpr::Args a;
+    a.x = logits; a.ld = ld; a.target = target; a.logprob = logprob; a.entropy = entropy; a.top_ids = top_ids; a.top_logprobs = top_logprobs;
+    a.V = vocab; a.mask_id = mask_id >= 0 && mask_id < vocab ? mask_id : -1; a.k = top_k;
+    // threads per row as for the confidence kernel: a batch of loads each, and at most the SMs' worth for all rows
+    const long long most = std::min<long long>(vocab * (long long)es / (16 * lpr::U), 1776LL * di.sm_count / rows);
+    int per_row = 128;
+    while (per_row < lpr::MAX_CL * lpr::MAX_THREADS && 2 * per_row <= most) per_row *= 2;
+    a.cl = std::min(lpr::MAX_CL, std::max(1, per_row / 256));
+    const int threads = std::min(lpr::MAX_THREADS, per_row / a.cl);
+    const long long blocks = (long long)rows * a.cl;
+    if (blocks > INT32_MAX) return POLESTAR_E_INVAL;
+    cudaStream_t st = (cudaStream_t)stream;
+    auto kern = dtype == POLESTAR_BF16 ? lpr::token_logprobs_kernel<__nv_bfloat16> : lpr::token_logprobs_kernel<float>;
+    if (a.cl > 1) CK(launch_k_cluster(kern, dim3((unsigned)blocks), dim3(threads), 0, st, (unsigned)a.cl, a));
+    else CK(launch_k(kern, dim3((unsigned)blocks), dim3(threads), 0, st, a));
+    return POLESTAR_OK;
+}
