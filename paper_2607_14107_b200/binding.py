@@ -37,7 +37,7 @@ EXPORTS = [
     "polestar_k_attention", "polestar_k_hidden_delta", "polestar_k_select",
     "polestar_k_refresh_scratch_bytes", "polestar_k_refresh", "polestar_k_confidence",
     "polestar_k_confidence_noalloc", "polestar_sm_count",
-    "polestar_k_fp4_scale_bytes", "polestar_k_fp4_quantize", "polestar_k_kv4_append", "polestar_k_token_logprobs",
+    "polestar_k_fp4_scale_bytes", "polestar_k_fp4_quantize", "polestar_k_fp4_matmul", "polestar_k_kv4_append", "polestar_k_token_logprobs",
 ]
 
 
@@ -145,6 +145,8 @@ def load():
     lib.polestar_k_fp4_scale_bytes.argtypes = [i64, i32, i32, i32]
     lib.polestar_k_fp4_quantize.restype = C.c_int
     lib.polestar_k_fp4_quantize.argtypes = [vp, i64, i32, i32, i32, i32, i32, vp, vp, vp, vp, vp]
+    lib.polestar_k_fp4_matmul.restype = C.c_int
+    lib.polestar_k_fp4_matmul.argtypes = [vp] * 7 + [i64] + [i32] * 5 + [vp]
     lib.polestar_k_kv4_append.restype = C.c_int
     lib.polestar_k_kv4_append.argtypes = [vp, vp, vp, vp] + [i32] * 6 + [vp] * 9
     lib.polestar_k_token_logprobs.restype = C.c_int
@@ -526,6 +528,23 @@ def polestar_k_fp4_quantize(x, codes, scales, fmt: int, layout: int = SCALES_ROW
     _buffer("deq", deq, x.dtype, (rows, d), optional=True)
     _check(load().polestar_k_fp4_quantize(_ptr(x), ld, rows, d, _dtype_code(x), fmt, layout, _ptr(tensor_scale), _ptr(codes), _ptr(scales),
                                           _ptr(deq), C.c_void_p(_stream())))
+
+
+def polestar_k_fp4_matmul(a_codes, a_scales, b_codes, b_scales, out, fmt: int, a_tensor_scale=None, b_tensor_scale=None):
+    """codes uint8 [M][K/2] and [N][K/2] with scales in the TILED layout -> out [M][N] (rows may be strided)."""
+    _need(a_codes.dim() == 2 and b_codes.dim() == 2, "codes have to be matrices")
+    (M, half), N = a_codes.shape, b_codes.shape[0]
+    _buffer("a_codes", a_codes, torch.uint8)
+    _buffer("b_codes", b_codes, torch.uint8, (N, half))
+    for name, t, rows in (("a_scales", a_scales, M), ("b_scales", b_scales, N)):
+        _buffer(name, t, torch.uint8)
+        _need(2 * half % 64 == 0 and t.numel() == polestar_k_fp4_scale_bytes(rows, 2 * half, fmt, SCALES_TILED), f"{name} has the wrong size")
+    for name, t in (("a_tensor_scale", a_tensor_scale), ("b_tensor_scale", b_tensor_scale)):
+        _buffer(name, t, torch.float32, (1,), optional=True)
+    ld = _row_stride("out", out)
+    _need(tuple(out.shape) == (M, N), f"out has the shape {tuple(out.shape)}, not {(M, N)}")
+    _check(load().polestar_k_fp4_matmul(_ptr(a_codes), _ptr(a_scales), _ptr(b_codes), _ptr(b_scales), _ptr(a_tensor_scale),
+                                        _ptr(b_tensor_scale), _ptr(out), ld, M, N, 2 * half, fmt, _dtype_code(out), C.c_void_p(_stream())))
 
 
 def _kv4_cache(kc, ks, vc, vs):

@@ -1,0 +1,229 @@
+// Product of two microscaled 4-bit matrices on 5th-generation tensor cores:  out[m][n] = ta tb sum_k A[m][k] B[n][k].
+//
+// tcgen05.mma with block scales multiplies E2M1 codes (64 of K per instruction, 128 bytes of a row are 256 of K) and takes the groups'
+// scales from tensor memory: rows of codes come by TMA (128-byte swizzle, as bf16 rows of the same bytes would), 512-byte blocks of
+// the tiled scales (128 rows x 4 groups) by plain bulk copies, and tcgen05.cp moves a block into four columns of tensor memory, copied to the
+// four lane quarters.  Products of codes and scales are exact, sums are the tensor core's fp32.
+#pragma once
+#include "fp4.cuh"
+#include "tcgen05.cuh"
+
+namespace ps {
+namespace fp4 {
+
+using namespace tc;
+
+constexpr int KB = 256;                          // K of a ring slot: one 128-byte row of codes
+constexpr uint32_t BLOCK_BYTES = 512;            // scales of 128 rows x 4 groups
+__host__ __device__ constexpr int scale_blocks(int fmt) { return KB / (4 * group(fmt)); }       // per slot and 128 rows: 4 or 2
+
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
+}
+// Shared-memory descriptor of a scale block: 32 rows of 16 bytes, no swizzle, 8-row groups 128 bytes apart.
+__device__ __forceinline__ uint64_t smem_desc_scales(uint32_t addr) {
+    return (uint64_t)((addr & 0x3FFFFu) >> 4) | ((uint64_t)(128u >> 4) << 32) | ((uint64_t)1 << 46);
+}
+__device__ __forceinline__ void copy_scales(uint32_t tmem, uint64_t desc) {
+    asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(tmem), "l"(desc) : "memory");
+}
+// Instruction descriptor: E2M1 x E2M1 -> fp32, both K-major; scales E4M3 (nv) or E8M0 (mx).  The latter take two of the four bytes of a
+// column per instruction, which two (0 or 2) is part of the descriptor.
+template <int FMT>
+__device__ __forceinline__ uint32_t instr_desc_fp4(int m, int n, uint32_t byte) {
+    return (byte << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(n >> 3) << 17) | ((FMT == MX ? 1u : 0u) << 23) | ((uint32_t)(m >> 7) << 27) | (byte << 29);
+}
+template <int FMT>
+__device__ __forceinline__ void umma_fp4(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t sa, uint32_t sb, uint32_t accumulate) {
+    if (FMT == NV)
+        asm volatile("{\n .reg .pred p;\n setp.ne.b32 p, %6, 0;\n"
+                     " tcgen05.mma.cta_group::1.kind::mxf4nvf4.block_scale.scale_vec::4X [%0], %1, %2, %3, [%4], [%5], p;\n}\n"
+                     ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(sa), "r"(sb), "r"(accumulate) : "memory");
+    else
+        asm volatile("{\n .reg .pred p;\n setp.ne.b32 p, %6, 0;\n"
+                     " tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n}\n"
+                     ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(sa), "r"(sb), "r"(accumulate) : "memory");
+}
+
+// After a wait that gave up: the copies of the last slots asked for land before their shared memory goes (bounded).
+__device__ __forceinline__ void drain_ring(int issued, int stages, uint32_t full0) {
+    for (int u = max(0, issued - stages); u < issued; ++u) {
+        const Ring r(u, stages);
+        const long long t0 = clock64();
+        while (!mbar_try_wait(full0 + 8u * (uint32_t)r.slot, r.phase) && clock64() - t0 < WAIT_LIMIT_CYCLES) {}
+    }
+}
+
+struct GemmArgs {
+    const uint8_t* as; const uint8_t* bs;        // tiled scales
+    const float* ta; const float* tb;            // factors of the tensors (null: 1)
+    void* out; long long ld;
+    int M, N, K;
+    int split;                                   // CTAs of a cluster that share the K of a tile
+};
+
+// ---- few rows of A: bound by the stream of B ---------------------------------------------------------------------------
+// The wide matrix takes the 128 lanes: D^T = B A^T, a tile is 128 columns of the output x T rows of it, so a few rows cost no padding of the
+// stream.  The CTAs of a cluster (up to eight, while that leaves SMs to fill) take consecutive parts of K; each then hands its partial sums to
+// the CTA that owns the output rows (through distributed shared memory), which adds them in the order of K.
+constexpr int ST_THREADS = 192;                  // TMA, MMA, four epilogue warps
+constexpr int ST_MAX_STAGES = 8;
+__host__ __device__ constexpr uint32_t st_stage_bytes(int T, int fmt) { return 128 * 128 + T * 128 + 2 * scale_blocks(fmt) * BLOCK_BYTES; }
+__host__ __device__ constexpr uint32_t st_exchange_bytes(int T) { return 128 * T * 4; }
+__host__ __device__ constexpr int st_stages(int T, int fmt) {
+    const int n = (int)((225 * 1024 - 1024 - st_exchange_bytes(T)) / st_stage_bytes(T, fmt));
+    return n < ST_MAX_STAGES ? n : ST_MAX_STAGES;
+}
+__host__ __device__ constexpr size_t st_smem_bytes(int T, int fmt) { return 1024 + (size_t)st_stages(T, fmt) * st_stage_bytes(T, fmt) + st_exchange_bytes(T); }
+
+template <int T, int FMT, typename OUT>
+__global__ void __launch_bounds__(ST_THREADS, 1)
+gemm_stream_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ GemmArgs g) {
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ uint64_t bars[2 * ST_MAX_STAGES + 1];
+    __shared__ uint32_t tmem_base_sh;
+    __shared__ int abort_sh;
+    constexpr int STAGES = st_stages(T, FMT), SB = scale_blocks(FMT);
+    constexpr uint32_t STAGE = st_stage_bytes(T, FMT);
+    constexpr uint32_t A_OFF = 128 * 128, BS_OFF = A_OFF + T * 128, AS_OFF = BS_OFF + SB * BLOCK_BYTES;
+    constexpr uint32_t COLS = 256, SF_COL = 128;          // accumulator: columns 0 .. T - 1; two sets of scales from column 128 on
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int rank = g.split > 1 ? (int)cluster_rank() : 0;
+    const int tile_n = (int)blockIdx.x / g.split, tile_m = blockIdx.y;
+    const int kb_total = (g.K + KB - 1) / KB;
+    const int kb0 = (int)((long long)kb_total * rank / g.split), kb1 = (int)((long long)kb_total * (rank + 1) / g.split);
+    const int sb_row = (g.K / group(FMT) + 3) / 4;        // scale blocks of 128 rows
+
+    uint8_t* smem = (uint8_t*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
+    const uint32_t smem_base = smem_u32(smem), bar0 = smem_u32(&bars[0]);
+    auto full = [&](int s) { return bar0 + 8u * (uint32_t)s; };
+    auto empty = [&](int s) { return bar0 + 8u * (uint32_t)(ST_MAX_STAGES + s); };
+    const uint32_t done = bar0 + 16u * ST_MAX_STAGES;
+    volatile int* abort_flag = &abort_sh;
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < STAGES; ++s) { mbar_init(full(s), 1); mbar_init(empty(s), 1); }
+        mbar_init(done, 1);
+        abort_sh = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    }
+    if (warp == 1) tmem_alloc(smem_u32(&tmem_base_sh), COLS);
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    pdl_trigger();
+    const uint32_t tmem = tmem_base_sh;
+    // (every CTA of the cluster runs before another one writes into its shared memory)
+    if (g.split > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
+
+    int issued = 0;                                       // ring slots that this thread has asked for
+    if (warp == 0) {
+        if (elect_one()) {
+            pdl_wait();
+            const uint64_t policy = l2_policy_evict_first();
+            bool ok = true;
+            Ring r(0, STAGES);
+            for (int kb = kb0; kb < kb1 && ok; ++kb, r.next(STAGES)) {
+                if (kb - kb0 >= STAGES) ok = mbar_wait(empty(r.slot), r.phase ^ 1u, abort_flag);
+                if (!ok) break;
+                const uint32_t slot = smem_base + (uint32_t)r.slot * STAGE;
+                const uint32_t sbytes = (uint32_t)min(SB, sb_row - kb * SB) * BLOCK_BYTES;
+                mbar_expect_tx(full(r.slot), 128 * 128 + T * 128 + 2 * sbytes);
+                if (gridDim.y == 1) tma_load_2d_hint(slot, &map_b, full(r.slot), kb * 128, tile_n * 128, policy);
+                else tma_load_2d(slot, &map_b, full(r.slot), kb * 128, tile_n * 128);
+                tma_load_2d(slot + A_OFF, &map_a, full(r.slot), kb * 128, tile_m * T);
+                bulk_load(slot + BS_OFF, g.bs + ((size_t)tile_n * sb_row + kb * SB) * BLOCK_BYTES, sbytes, full(r.slot));
+                bulk_load(slot + AS_OFF, g.as + ((size_t)(tile_m * T / 128) * sb_row + kb * SB) * BLOCK_BYTES, sbytes, full(r.slot));
+                ++issued;
+            }
+        }
+    } else if (warp == 1) {
+        if (elect_one()) {
+            bool ok = true;
+            Ring r(0, STAGES);
+            for (int kb = kb0; kb < kb1 && ok; ++kb, r.next(STAGES)) {
+                ok = mbar_wait(full(r.slot), r.phase, abort_flag);
+                if (!ok) break;
+                tc_fence_after();
+                const uint32_t slot = smem_base + (uint32_t)r.slot * STAGE;
+                const int steps = min(4, (g.K - kb * KB) / 64), blocks = min(SB, sb_row - kb * SB);
+                const uint32_t sf_b = tmem + SF_COL + (uint32_t)(kb & 1) * 32u, sf_a = sf_b + 16u;
+                for (int c = 0; c < blocks; ++c) {
+                    copy_scales(sf_b + 4u * (uint32_t)c, smem_desc_scales(slot + BS_OFF + (uint32_t)c * BLOCK_BYTES));
+                    copy_scales(sf_a + 4u * (uint32_t)c, smem_desc_scales(slot + AS_OFF + (uint32_t)c * BLOCK_BYTES));
+                }
+                const uint64_t db = smem_desc_sw128(slot), da = smem_desc_sw128(slot + A_OFF);
+                for (int s = 0; s < steps; ++s) {
+                    const uint32_t c = 4u * (uint32_t)(FMT == NV ? s : s >> 1), byte = FMT == NV ? 0u : (uint32_t)(s & 1) * 2u;
+                    umma_fp4<FMT>(tmem, db + (uint64_t)(2 * s), da + (uint64_t)(2 * s), instr_desc_fp4<FMT>(128, T, byte), sf_b + c, sf_a + c, kb > kb0 || s > 0 ? 1u : 0u);
+                }
+                umma_commit(empty(r.slot));
+            }
+            umma_commit(done);      // (also on failure: the epilogue then sees the abort flag)
+        }
+    }
+    __syncwarp();
+    // ---- epilogue: tensor-memory lane = output column, accumulator column = output row ----
+    const int quarter = warp & 3;
+    const uint32_t lane_base = tmem + ((uint32_t)(quarter * 32) << 16);
+    const int rows_each = T / g.split;                    // output rows that this CTA finishes
+    float* ex = reinterpret_cast<float*>(smem + (size_t)STAGES * STAGE);
+    bool ok = true;
+    if (warp >= 2) {
+        ok = mbar_wait(done, 0, abort_flag) && !*abort_flag;
+        ok = __all_sync(0xffffffffu, ok) != 0;
+        tc_fence_after();
+    }
+    const int n = tile_n * 128 + quarter * 32 + lane;
+    float scale = 1.f;
+    if (warp >= 2) {
+        pdl_wait();
+        scale = (g.ta ? __ldg(g.ta) : 1.f) * (g.tb ? __ldg(g.tb) : 1.f);
+        if (!ok) scale = __uint_as_float(0x7fc00000u);    // a bounded wait gave up: NaN, not a partial sum
+    }
+    auto store = [&](int m, float v) {
+        if (m < g.M && n < g.N) ((OUT*)g.out)[(size_t)m * g.ld + n] = from_f<OUT>(v * scale);
+    };
+    if (g.split == 1) {
+        if (warp >= 2)
+            for (int c = 0; c < T; c += 16) {
+                float v[16];
+                tmem_ld16(lane_base + (uint32_t)c, v);
+#pragma unroll
+                for (int i = 0; i < 16; ++i) store(tile_m * T + c + i, v[i]);
+            }
+    } else {
+        asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+        if (warp >= 2)
+            for (int c = 0; c < T; c += 16) {
+                float v[16];
+                tmem_ld16(lane_base + (uint32_t)c, v);
+                if (kb0 >= kb1 || !ok) {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) v[i] = ok ? 0.f : __uint_as_float(0x7fc00000u);
+                }
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const int owner = (c + i) / rows_each, at = (c + i) - owner * rows_each;
+                    const uint32_t dst = dsmem_addr(smem_u32(ex + (rank * rows_each + at) * 128 + quarter * 32 + lane), (uint32_t)owner);
+                    asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(dst), "f"(v[i]) : "memory");
+                }
+            }
+        __syncwarp();
+        cluster_sync_all();
+        if (warp >= 2)
+            for (int i = 0; i < rows_each; ++i) {
+                float v = 0.f;
+                for (int s = 0; s < g.split; ++s) v += ex[(s * rows_each + i) * 128 + quarter * 32 + lane];
+                store(tile_m * T + rank * rows_each + i, v);
+            }
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (abort_sh && issued > 0) drain_ring(issued, STAGES, bar0);
+    if (warp == 1) tmem_dealloc(tmem, COLS);
+}
+
+}  // namespace fp4
+}  // namespace ps

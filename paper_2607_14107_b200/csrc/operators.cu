@@ -6,10 +6,12 @@
 #include <cuda_runtime.h>
 
 #include <algorithm>
+#include <atomic>
 #include <climits>
 #include <mutex>
 
 #include "fp4.cuh"
+#include "fp4_gemm.cuh"
 #include "logprobs.cuh"
 
 using namespace ps;
@@ -22,6 +24,7 @@ struct DevInfo { bool ready = false; int sm_count = 0; };
 static const int MAX_DEVICES = 64;
 static std::mutex g_mu;
 static DevInfo g_dev[MAX_DEVICES];
+static cudaError_t set_kernel_attributes();
 static int device_info(DevInfo* out) {
     int dev = 0;
     CK(cudaGetDevice(&dev));
@@ -30,6 +33,7 @@ static int device_info(DevInfo* out) {
     DevInfo& di = g_dev[dev];
     if (!di.ready) {
         CK(cudaDeviceGetAttribute(&di.sm_count, cudaDevAttrMultiProcessorCount, dev));
+        CK(set_kernel_attributes());
         di.ready = true;
     }
     *out = di;
@@ -83,6 +87,79 @@ extern "C" int polestar_k_fp4_quantize(const void* x, int64_t ld_x, int32_t rows
     if (dtype == POLESTAR_BF16) CK(nv ? (launch_quantize<__nv_bfloat16, fp4::NV>(a, di.sm_count, st)) : (launch_quantize<__nv_bfloat16, fp4::MX>(a, di.sm_count, st)));
     else CK(nv ? (launch_quantize<float, fp4::NV>(a, di.sm_count, st)) : (launch_quantize<float, fp4::MX>(a, di.sm_count, st)));
     return POLESTAR_OK;
+}
+
+typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
+                                  const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
+                                  CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+static EncodeTiledFn get_encode_fn() {
+    static std::atomic<EncodeTiledFn> fn{nullptr};
+    EncodeTiledFn f = fn.load();
+    if (!f) {
+        void* p = nullptr;
+        cudaDriverEntryPointQueryResult qres;
+        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &qres) == cudaSuccess && qres == cudaDriverEntryPointSuccess) {
+            f = (EncodeTiledFn)p;
+            fn.store(f);
+        }
+    }
+    return f;
+}
+// rows of codes, [rows][bytes] with bytes % 16 == 0: boxes of 128 bytes x box_rows, 128-byte swizzle; what lies outside arrives as zeros
+static bool make_code_map(CUtensorMap* out, const void* base, uint64_t rows, uint64_t bytes, uint32_t box_rows) {
+    EncodeTiledFn fn = get_encode_fn();
+    if (!fn) return false;
+    cuuint64_t dims[2] = {bytes, rows};
+    cuuint64_t strides[1] = {bytes};
+    cuuint32_t box[2] = {128, box_rows};
+    cuuint32_t estr[2] = {1, 1};
+    return fn(out, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int T, int FMT, typename OUT>
+static int launch_gemm_stream(const uint8_t* a, const uint8_t* b, fp4::GemmArgs g, int sms, cudaStream_t st) {
+    CUtensorMap ma, mb;
+    if (!make_code_map(&ma, a, g.M, g.K / 2, T) || !make_code_map(&mb, b, g.N, g.K / 2, 128)) return POLESTAR_E_CUDA;
+    const long long tiles_n = ((long long)g.N + 127) / 128, tiles_m = ((long long)g.M + T - 1) / T;
+    const int kbs = (g.K + fp4::KB - 1) / fp4::KB;
+    // a cluster over K while its CTAs have an SM each and two slots' worth of K
+    g.split = 1;
+    while (g.split < 8 && tiles_n * tiles_m * g.split * 2 <= sms && g.split * 4 <= kbs) g.split *= 2;
+    if (tiles_m > 65535 || tiles_n * g.split > INT32_MAX) return POLESTAR_E_INVAL;
+    const dim3 grid((unsigned)(tiles_n * g.split), (unsigned)tiles_m);
+    const size_t smem = fp4::st_smem_bytes(T, FMT);
+    if (g.split > 1) CK(launch_k_cluster(fp4::gemm_stream_kernel<T, FMT, OUT>, grid, dim3(fp4::ST_THREADS), smem, st, (unsigned)g.split, ma, mb, g));
+    else CK(launch_k(fp4::gemm_stream_kernel<T, FMT, OUT>, grid, dim3(fp4::ST_THREADS), smem, st, ma, mb, g));
+    return POLESTAR_OK;
+}
+template <int FMT, typename OUT>
+static int launch_gemm_fp4(const uint8_t* a, const uint8_t* b, const fp4::GemmArgs& g, int sms, cudaStream_t st) {
+    if (g.M <= 32) return launch_gemm_stream<32, FMT, OUT>(a, b, g, sms, st);
+    if (g.M <= 64) return launch_gemm_stream<64, FMT, OUT>(a, b, g, sms, st);
+    return launch_gemm_stream<128, FMT, OUT>(a, b, g, sms, st);
+}
+
+extern "C" int polestar_k_fp4_matmul(const uint8_t* a_codes, const uint8_t* a_scales, const uint8_t* b_codes, const uint8_t* b_scales,
+                                     const float* a_tensor_scale, const float* b_tensor_scale, void* out, int64_t ld_out, int32_t M,
+                                     int32_t N, int32_t K, int32_t format, int32_t out_dtype, void* stream) {
+    if (M < 0 || N < 0 || K <= 0 || K % 64 || ld_out < N || !fp4_format_ok(format, POLESTAR_SCALES_TILED)) return POLESTAR_E_INVAL;
+    if (out_dtype != POLESTAR_F32 && out_dtype != POLESTAR_BF16) return POLESTAR_E_INVAL;
+    if (M == 0 || N == 0) return POLESTAR_OK;    // nothing to compute (the pointers may be null)
+    if (!a_codes || !a_scales || !b_codes || !b_scales || !out) return POLESTAR_E_INVAL;
+    if (((uintptr_t)a_codes | (uintptr_t)a_scales | (uintptr_t)b_codes | (uintptr_t)b_scales) & 15) return POLESTAR_E_INVAL;
+    if (((uintptr_t)out & (out_dtype == POLESTAR_BF16 ? 1 : 3)) || (((uintptr_t)a_tensor_scale | (uintptr_t)b_tensor_scale) & 3)) return POLESTAR_E_INVAL;
+    DevInfo di;
+    int rc = device_info(&di);
+    if (rc) return rc;
+    fp4::GemmArgs g;
+    g.as = a_scales; g.bs = b_scales; g.ta = a_tensor_scale; g.tb = b_tensor_scale; g.out = out; g.ld = ld_out;
+    g.M = M; g.N = N; g.K = K; g.split = 1;
+    cudaStream_t st = (cudaStream_t)stream;
+    const bool nv = format == POLESTAR_FP4_NV;
+    if (out_dtype == POLESTAR_BF16)
+        return nv ? launch_gemm_fp4<fp4::NV, __nv_bfloat16>(a_codes, b_codes, g, di.sm_count, st) : launch_gemm_fp4<fp4::MX, __nv_bfloat16>(a_codes, b_codes, g, di.sm_count, st);
+    return nv ? launch_gemm_fp4<fp4::NV, float>(a_codes, b_codes, g, di.sm_count, st) : launch_gemm_fp4<fp4::MX, float>(a_codes, b_codes, g, di.sm_count, st);
 }
 
 // A cache of keys and values in 4 bits: what append and attention accept of its geometry.
@@ -149,4 +226,20 @@ extern "C" int polestar_k_token_logprobs(const void* logits, int64_t ld, int32_t
     if (a.cl > 1) CK(launch_k_cluster(kern, dim3((unsigned)blocks), dim3(threads), 0, st, (unsigned)a.cl, a));
     else CK(launch_k(kern, dim3((unsigned)blocks), dim3(threads), 0, st, a));
     return POLESTAR_OK;
+}
+
+// kernels with more shared memory than the default limit
+template <int T, int FMT>
+static cudaError_t stream_attributes() {
+    const int n = (int)fp4::st_smem_bytes(T, FMT);
+    cudaError_t e = cudaFuncSetAttribute(fp4::gemm_stream_kernel<T, FMT, float>, cudaFuncAttributeMaxDynamicSharedMemorySize, n);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(fp4::gemm_stream_kernel<T, FMT, __nv_bfloat16>, cudaFuncAttributeMaxDynamicSharedMemorySize, n);
+    return e;
+}
+static cudaError_t set_kernel_attributes() {
+    cudaError_t e;
+    if ((e = stream_attributes<32, fp4::NV>()) != cudaSuccess || (e = stream_attributes<64, fp4::NV>()) != cudaSuccess) return e;
+    if ((e = stream_attributes<128, fp4::NV>()) != cudaSuccess || (e = stream_attributes<32, fp4::MX>()) != cudaSuccess) return e;
+    if ((e = stream_attributes<64, fp4::MX>()) != cudaSuccess || (e = stream_attributes<128, fp4::MX>()) != cudaSuccess) return e;
+    return cudaSuccess;
 }
