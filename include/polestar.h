@@ -440,6 +440,22 @@ int polestar_k_kv4_append(const void *k_dev, const void *v_dev, const int32_t *i
                           const float *v_scale_dev, uint8_t *kc_dev, uint8_t *ks_dev, uint8_t *vc_dev, uint8_t *vs_dev,
                           void *k_deq_dev, void *v_deq_dev, void *cuda_stream);
 
+/* Attention of query rows over that cache (Eq. 3 without the drift of stored rows; bidirectional: every row sees every key of its sequence):
+ *   s_j = q . k_j / sqrt(head_dim) for j < len,  out = sum_j softmax(s)_j v_j,  lse = log sum_j e^(s_j)
+ * with keys and values as the cache stores them (exact; bf16: probabilities rounded to 16 bits, fp32: to 22), fp32 sums.
+ *   q_dev [batch][R][n_heads*head_dim], out_dev the same, F32 or BF16; query head h reads K/V head h / (n_heads / n_kv)
+ *   lens_dev int32 [batch]: keys of every sequence (NULL: cap; clamped to 0 .. cap); cache rows behind them are not read
+ *   lse_dev float [batch][R][n_heads] (natural logarithm; NULL: skipped), to join the rows with attention over other keys
+ * A sequence without keys gives zero rows and lse = -inf.  head_dim 64 or 128, n_heads <= 1024.
+ *   scratch_dev: >= polestar_k_kv4_scratch_bytes(...) bytes, of one call at a time.
+ * q, out, the cache's four arrays and scratch 16-byte aligned. */
+size_t polestar_k_kv4_scratch_bytes(int32_t batch, int32_t R, int32_t cap, int32_t n_heads, int32_t n_kv, int32_t head_dim);
+int polestar_k_kv4_attention(const void *q_dev, const uint8_t *kc_dev, const uint8_t *ks_dev, const uint8_t *vc_dev,
+                             const uint8_t *vs_dev, const float *k_scale_dev, const float *v_scale_dev, const int32_t *lens_dev,
+                             void *out_dev, float *lse_dev, int32_t batch, int32_t R, int32_t cap, int32_t n_heads,
+                             int32_t n_kv, int32_t head_dim, int32_t dtype, void *scratch_dev, size_t scratch_bytes,
+                             void *cuda_stream);
+
 /* Log-probability of a given token, entropy and the most likely alternatives of logits rows (the quantities next to the
  * confidence of Eq. 1 that samplers commit by and servers report; the softmax runs over the full vocabulary).
  *   logits_dev [rows][vocab], F32 or BF16, row stride ld elements (>= vocab), any alignment of the element's size

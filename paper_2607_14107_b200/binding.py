@@ -37,7 +37,8 @@ EXPORTS = [
     "polestar_k_attention", "polestar_k_hidden_delta", "polestar_k_select",
     "polestar_k_refresh_scratch_bytes", "polestar_k_refresh", "polestar_k_confidence",
     "polestar_k_confidence_noalloc", "polestar_sm_count",
-    "polestar_k_fp4_scale_bytes", "polestar_k_fp4_quantize", "polestar_k_fp4_matmul", "polestar_k_kv4_append", "polestar_k_token_logprobs",
+    "polestar_k_fp4_scale_bytes", "polestar_k_fp4_quantize", "polestar_k_fp4_matmul", "polestar_k_kv4_append",
+    "polestar_k_kv4_scratch_bytes", "polestar_k_kv4_attention", "polestar_k_token_logprobs",
 ]
 
 
@@ -149,6 +150,10 @@ def load():
     lib.polestar_k_fp4_matmul.argtypes = [vp] * 7 + [i64] + [i32] * 5 + [vp]
     lib.polestar_k_kv4_append.restype = C.c_int
     lib.polestar_k_kv4_append.argtypes = [vp, vp, vp, vp] + [i32] * 6 + [vp] * 9
+    lib.polestar_k_kv4_scratch_bytes.restype = sz
+    lib.polestar_k_kv4_scratch_bytes.argtypes = [i32] * 6
+    lib.polestar_k_kv4_attention.restype = C.c_int
+    lib.polestar_k_kv4_attention.argtypes = [vp] * 10 + [i32] * 7 + [vp, sz, vp]
     lib.polestar_k_token_logprobs.restype = C.c_int
     lib.polestar_k_token_logprobs.argtypes = [vp, i64, i32, i32, i32, vp, i32, i32, vp, vp, vp, vp, vp]
     _lib = lib
@@ -572,6 +577,27 @@ def polestar_k_kv4_append(k, v, idx, counts, kc, ks, vc, vs, k_scale=None, v_sca
     _check(load().polestar_k_kv4_append(_ptr(k), _ptr(v), _ptr(idx), _ptr(counts), b, R, cap, n_kv, dh, _dtype_code(k), _ptr(k_scale),
                                         _ptr(v_scale), _ptr(kc), _ptr(ks), _ptr(vc), _ptr(vs), _ptr(k_deq), _ptr(v_deq),
                                         C.c_void_p(_stream())))
+
+
+def polestar_k_kv4_scratch_bytes(batch, R, cap, n_heads, n_kv_heads, head_dim) -> int:
+    return int(load().polestar_k_kv4_scratch_bytes(batch, R, cap, n_heads, n_kv_heads, head_dim))
+
+
+def polestar_k_kv4_attention(q, kc, ks, vc, vs, k_scale, v_scale, lens, out, lse, scratch):
+    """q, out [batch][R][n_heads*head_dim], lse [batch][R][n_heads] (None: skipped), lens int32 [batch] (None: the whole cache)."""
+    b, cap, n_kv, dh = _kv4_cache(kc, ks, vc, vs)
+    _need(q.dim() == 3 and q.shape[2] % dh == 0, "q has to be [batch][R][n_heads*head_dim]")
+    R, n_heads = q.shape[1], q.shape[2] // dh
+    _buffer("q", q, q.dtype, (b, R, n_heads * dh))
+    _buffer("out", out, q.dtype, q.shape)
+    _buffer("lse", lse, torch.float32, (b, R, n_heads), optional=True)
+    _buffer("lens", lens, torch.int32, (b,), optional=True)
+    for name, t in (("k_scale", k_scale), ("v_scale", v_scale)):
+        _buffer(name, t, torch.float32, (1,), optional=True)
+    _buffer("scratch", scratch, torch.uint8)
+    _check(load().polestar_k_kv4_attention(_ptr(q), _ptr(kc), _ptr(ks), _ptr(vc), _ptr(vs), _ptr(k_scale), _ptr(v_scale), _ptr(lens), _ptr(out),
+                                           _ptr(lse), b, R, cap, n_heads, n_kv, dh, _dtype_code(q), _ptr(scratch), scratch.numel(),
+                                           C.c_void_p(_stream())))
 
 
 def polestar_k_token_logprobs(logits, target, mask_id, logprob, entropy, top_ids=None, top_logprobs=None):

@@ -8,10 +8,12 @@
 #include <algorithm>
 #include <atomic>
 #include <climits>
+#include <cmath>
 #include <mutex>
 
 #include "fp4.cuh"
 #include "fp4_gemm.cuh"
+#include "kv4_attn.cuh"
 #include "logprobs.cuh"
 
 using namespace ps;
@@ -192,6 +194,59 @@ extern "C" int polestar_k_kv4_append(const void* k, const void* v, const int32_t
     if (dtype == POLESTAR_BF16) CK(launch_k(fp4::kv_append_kernel<__nv_bfloat16>, grid, dim3(fp4::THREADS), 0, (cudaStream_t)stream, a));
     else CK(launch_k(fp4::kv_append_kernel<float>, grid, dim3(fp4::THREADS), 0, (cudaStream_t)stream, a));
     return POLESTAR_OK;
+}
+
+// Parts that the keys are split into: enough CTAs for three on every SM of a B200, no part shorter than four chunks a warp.  A function of the
+// sizes alone, so that a scratch of polestar_k_kv4_scratch_bytes() bytes suffices for every call of these sizes.
+static int kv4_split(long long batch, long long R, int cap, int n_heads, int n_kv) {
+    const long long tiles = (R * (n_heads / n_kv) + kv4::ROWS - 1) / kv4::ROWS, base = batch * n_kv * tiles;
+    const long long most = std::max<long long>(1, cap / (4 * kv4::CHUNK * kv4::WARPS));
+    return (int)std::max<long long>(1, std::min<long long>(std::min<long long>(kv4::MAX_SPLIT, most), 3 * 148 / std::max<long long>(base, 1)));
+}
+static bool kv4_attention_shape_ok(int batch, int R, int cap, int n_heads, int n_kv, int head_dim) {
+    return kv4_shape_ok(batch, R, cap, n_kv, head_dim) && R <= 65536 && n_heads > 0 && n_heads <= 1024 && n_heads % n_kv == 0;
+}
+
+extern "C" size_t polestar_k_kv4_scratch_bytes(int32_t batch, int32_t R, int32_t cap, int32_t n_heads, int32_t n_kv, int32_t head_dim) {
+    if (!kv4_attention_shape_ok(batch, R, cap, n_heads, n_kv, head_dim)) return 0;
+    const size_t rows = (size_t)batch * R * n_heads;
+    const int split = kv4_split(batch, R, cap, n_heads, n_kv);
+    return 256 + (split > 1 ? split * rows * ((size_t)head_dim * 4 + 8) : 0);
+}
+
+template <typename T, int DH>
+static int launch_kv4_warp(const kv4::Args& a, int batch, cudaStream_t st) {
+    const long long tiles = ((long long)a.R * (a.n_heads / a.n_kv) + kv4::ROWS - 1) / kv4::ROWS;
+    if (tiles * a.split > INT32_MAX) return POLESTAR_E_INVAL;
+    CK(launch_k(kv4::kv4_attn_warp_kernel<T, DH>, dim3((unsigned)(tiles * a.split), a.n_kv, batch), dim3(kv4::THREADS), 0, st, a));
+    if (a.split > 1) CK(launch_k(kv4::kv4_attn_join_kernel<T, DH>, dim3((unsigned)((a.rows_total + 7) / 8)), dim3(256), 0, st, a));
+    return POLESTAR_OK;
+}
+
+extern "C" int polestar_k_kv4_attention(const void* q, const uint8_t* kc, const uint8_t* ks, const uint8_t* vc, const uint8_t* vs,
+                                        const float* k_scale, const float* v_scale, const int32_t* lens, void* out, float* lse,
+                                        int32_t batch, int32_t R, int32_t cap, int32_t n_heads, int32_t n_kv, int32_t head_dim,
+                                        int32_t dtype, void* scratch, size_t scratch_bytes, void* stream) {
+    if (!kv4_attention_shape_ok(batch, R, cap, n_heads, n_kv, head_dim)) return POLESTAR_E_INVAL;
+    if (dtype != POLESTAR_F32 && dtype != POLESTAR_BF16) return POLESTAR_E_INVAL;
+    if (batch == 0 || R == 0) return POLESTAR_OK;         // no rows: nothing to do (the pointers may be null)
+    if (!q || !kc || !ks || !vc || !vs || !out || !scratch) return POLESTAR_E_INVAL;
+    if (((uintptr_t)q | (uintptr_t)out | (uintptr_t)kc | (uintptr_t)vc | (uintptr_t)ks | (uintptr_t)vs | (uintptr_t)scratch) & 15) return POLESTAR_E_INVAL;
+    if (((uintptr_t)k_scale | (uintptr_t)v_scale | (uintptr_t)lens | (uintptr_t)lse) & 3) return POLESTAR_E_INVAL;
+    if (scratch_bytes < polestar_k_kv4_scratch_bytes(batch, R, cap, n_heads, n_kv, head_dim)) return POLESTAR_E_NOSPACE;
+    DevInfo di;
+    int rc = device_info(&di);
+    if (rc) return rc;
+    kv4::Args a;
+    a.q = q; a.out = out; a.lse = lse; a.kc = kc; a.ks = ks; a.vc = vc; a.vs = vs; a.tk = k_scale; a.tv = v_scale; a.lens = lens;
+    a.R = R; a.cap = cap; a.n_heads = n_heads; a.n_kv = n_kv; a.rows_total = (long long)batch * R * n_heads;
+    a.split = kv4_split(batch, R, cap, n_heads, n_kv);
+    a.part_o = (float*)scratch;
+    a.part_ml = (float2*)((char*)scratch + (size_t)a.split * a.rows_total * head_dim * 4);
+    a.scale = 1.0f / sqrtf((float)head_dim);
+    cudaStream_t st = (cudaStream_t)stream;
+    if (dtype == POLESTAR_BF16) return head_dim == 128 ? launch_kv4_warp<__nv_bfloat16, 128>(a, batch, st) : launch_kv4_warp<__nv_bfloat16, 64>(a, batch, st);
+    return head_dim == 128 ? launch_kv4_warp<float, 128>(a, batch, st) : launch_kv4_warp<float, 64>(a, batch, st);
 }
 
 // ------------------------------------------------------------------------------------------
