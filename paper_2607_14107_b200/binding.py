@@ -490,28 +490,55 @@ SCALES_ROWS, SCALES_TILED = 0, 1
 LOGPROBS_MAX_TOP = 32
 
 
-def _need(ok: bool, msg: str) -> None:
-    if not ok:
-        raise PolestarError(E_INVAL, msg)
+# The checks below run on every call and cost more than a small kernel does if they are not kept short: messages are put together
+# only for a refusal, and addresses go to ctypes as plain integers.
+
+def _refuse(msg: str):
+    raise PolestarError(E_INVAL, msg)
 
 
-def _buffer(name: str, t: Optional[torch.Tensor], dtype, shape=None, optional: bool = False) -> None:
-    """A dense tensor of this type (and shape) on the current device: the library gets its address only."""
+def _device(name: str, t: torch.Tensor) -> int:
+    """The current CUDA device, which this tensor has to be on."""
+    dev = t.get_device()
+    if dev < 0 or dev != torch._C._cuda_getDevice():
+        _refuse(f"{name} is on {t.device}, not on the current CUDA device")
+    return dev
+
+
+def _raw_stream(dev: int) -> int:
+    return torch._C._cuda_getCurrentRawStream(dev)
+
+
+def _address(name: str, t: Optional[torch.Tensor], dtype, dev: int, shape=None, optional: bool = False) -> int:
+    """Address of a dense tensor of this type (and shape) on the current device: the library gets nothing else of it."""
     if t is None:
-        _need(optional, f"{name} is missing")
-        return
-    _need(t.is_cuda and t.device.index == torch.cuda.current_device(), f"{name} is on {t.device}, not on the current CUDA device")
-    _need(t.dtype == dtype, f"{name} has the type {t.dtype}, not {dtype}")
-    _need(shape is None or tuple(t.shape) == tuple(shape), f"{name} has the shape {tuple(t.shape)}, not {tuple(shape or ())}")
-    _need(t.is_contiguous(), f"{name} is not contiguous")
+        return 0 if optional else _refuse(f"{name} is missing")
+    if t.get_device() != dev:
+        _refuse(f"{name} is on {t.device}, not on the current CUDA device")
+    if t.dtype is not dtype:
+        _refuse(f"{name} has the type {t.dtype}, not {dtype}")
+    if shape is not None and t.shape != shape:
+        _refuse(f"{name} has the shape {tuple(t.shape)}, not {tuple(shape)}")
+    if not t.is_contiguous():
+        _refuse(f"{name} is not contiguous")
+    return t.data_ptr()
 
 
-def _row_stride(name: str, t: torch.Tensor) -> int:
-    """Elements between the rows of a matrix whose rows are dense."""
-    _need(t.is_cuda and t.device.index == torch.cuda.current_device(), f"{name} is on {t.device}, not on the current CUDA device")
-    _need(t.dim() == 2, f"{name} has {t.dim()} dimensions, not 2")
-    _need(t.shape[1] <= 1 or t.stride(1) == 1, f"{name} has rows that are not dense")
-    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+def _factor(name: str, t: Optional[torch.Tensor], dev: int) -> int:
+    return 0 if t is None else _address(name, t, torch.float32, dev, (1,))
+
+
+def _row_stride(name: str, t: torch.Tensor, dev: int) -> int:
+    """Elements between the rows of a matrix on this device whose rows are dense."""
+    if t.get_device() != dev:
+        _refuse(f"{name} is on {t.device}, not on the current CUDA device")
+    if t.dim() != 2:
+        _refuse(f"{name} has {t.dim()} dimensions, not 2")
+    rows, n = t.shape
+    stride = t.stride()
+    if n > 1 and stride[1] != 1:
+        _refuse(f"{name} has rows that are not dense")
+    return stride[0] if rows > 1 else n
 
 
 def fp4_group(fmt: int) -> int:
@@ -524,59 +551,62 @@ def polestar_k_fp4_scale_bytes(rows: int, d: int, fmt: int, layout: int) -> int:
 
 def polestar_k_fp4_quantize(x, codes, scales, fmt: int, layout: int = SCALES_ROWS, tensor_scale=None, deq=None):
     """x [rows][d] (rows may be strided) -> codes uint8 [rows][d/2], scales uint8 of polestar_k_fp4_scale_bytes() bytes, deq like x."""
-    ld = _row_stride("x", x)
+    dev = _device("x", x)
+    ld = _row_stride("x", x, dev)
     rows, d = x.shape
-    _buffer("codes", codes, torch.uint8, (rows, d // 2))
-    _buffer("scales", scales, torch.uint8)
-    _need(d % 32 == 0 and scales.numel() == polestar_k_fp4_scale_bytes(rows, d, fmt, layout), "scales have the wrong size for these rows")
-    _buffer("tensor_scale", tensor_scale, torch.float32, (1,), optional=True)
-    _buffer("deq", deq, x.dtype, (rows, d), optional=True)
-    _check(load().polestar_k_fp4_quantize(_ptr(x), ld, rows, d, _dtype_code(x), fmt, layout, _ptr(tensor_scale), _ptr(codes), _ptr(scales),
-                                          _ptr(deq), C.c_void_p(_stream())))
+    lib = load()
+    if d % 32 or scales.numel() != lib.polestar_k_fp4_scale_bytes(rows, d, fmt, layout):
+        _refuse(f"scales have {scales.numel()} bytes, which is not what {rows} rows of {d} channels take")
+    _check(lib.polestar_k_fp4_quantize(
+        x.data_ptr(), ld, rows, d, _dtype_code(x), fmt, layout, _factor("tensor_scale", tensor_scale, dev),
+        _address("codes", codes, torch.uint8, dev, (rows, d // 2)), _address("scales", scales, torch.uint8, dev),
+        _address("deq", deq, x.dtype, dev, (rows, d), optional=True), _raw_stream(dev)))
 
 
 def polestar_k_fp4_matmul(a_codes, a_scales, b_codes, b_scales, out, fmt: int, a_tensor_scale=None, b_tensor_scale=None):
     """codes uint8 [M][K/2] and [N][K/2] with scales in the TILED layout -> out [M][N] (rows may be strided)."""
-    _need(a_codes.dim() == 2 and b_codes.dim() == 2, "codes have to be matrices")
+    dev = _device("a_codes", a_codes)
+    if a_codes.dim() != 2 or b_codes.dim() != 2:
+        _refuse("codes have to be matrices")
     (M, half), N = a_codes.shape, b_codes.shape[0]
-    _buffer("a_codes", a_codes, torch.uint8)
-    _buffer("b_codes", b_codes, torch.uint8, (N, half))
-    for name, t, rows in (("a_scales", a_scales, M), ("b_scales", b_scales, N)):
-        _buffer(name, t, torch.uint8)
-        _need(2 * half % 64 == 0 and t.numel() == polestar_k_fp4_scale_bytes(rows, 2 * half, fmt, SCALES_TILED), f"{name} has the wrong size")
-    for name, t in (("a_tensor_scale", a_tensor_scale), ("b_tensor_scale", b_tensor_scale)):
-        _buffer(name, t, torch.float32, (1,), optional=True)
-    ld = _row_stride("out", out)
-    _need(tuple(out.shape) == (M, N), f"out has the shape {tuple(out.shape)}, not {(M, N)}")
-    _check(load().polestar_k_fp4_matmul(_ptr(a_codes), _ptr(a_scales), _ptr(b_codes), _ptr(b_scales), _ptr(a_tensor_scale),
-                                        _ptr(b_tensor_scale), _ptr(out), ld, M, N, 2 * half, fmt, _dtype_code(out), C.c_void_p(_stream())))
+    lib = load()
+    size = lib.polestar_k_fp4_scale_bytes
+    if half % 32 or a_scales.numel() != size(M, 2 * half, fmt, SCALES_TILED) or b_scales.numel() != size(N, 2 * half, fmt, SCALES_TILED):
+        _refuse(f"scales have {a_scales.numel()} and {b_scales.numel()} bytes, which is not what {M} and {N} rows of {2 * half} channels take")
+    ld = _row_stride("out", out, dev)
+    if out.shape != (M, N):
+        _refuse(f"out has the shape {tuple(out.shape)}, not {(M, N)}")
+    u8 = torch.uint8
+    _check(lib.polestar_k_fp4_matmul(
+        _address("a_codes", a_codes, u8, dev), _address("a_scales", a_scales, u8, dev), _address("b_codes", b_codes, u8, dev, (N, half)),
+        _address("b_scales", b_scales, u8, dev), _factor("a_tensor_scale", a_tensor_scale, dev), _factor("b_tensor_scale", b_tensor_scale, dev),
+        out.data_ptr(), ld, M, N, 2 * half, fmt, _dtype_code(out), _raw_stream(dev)))
 
 
-def _kv4_cache(kc, ks, vc, vs):
-    """Shape of a 4-bit K/V cache: batch, cap, n_kv, head_dim."""
-    _need(kc.dim() == 4, "kc has to be [batch][cap][n_kv][head_dim/2]")
-    b, cap, n_kv, half = kc.shape
-    for name, t, shape in (("kc", kc, kc.shape), ("vc", vc, kc.shape), ("ks", ks, (b, cap, n_kv, half // 8)), ("vs", vs, (b, cap, n_kv, half // 8))):
-        _buffer(name, t, torch.uint8, shape)
-    return b, cap, n_kv, 2 * half
+def _kv4_cache(kc, ks, vc, vs, dev):
+    """Geometry (batch, cap, n_kv, head_dim) and addresses of a 4-bit K/V cache."""
+    if kc.dim() != 4:
+        _refuse("kc has to be [batch][cap][n_kv][head_dim/2]")
+    shape, u8 = kc.shape, torch.uint8
+    b, cap, n_kv, half = shape
+    small = (b, cap, n_kv, half // 8)
+    return (b, cap, n_kv, 2 * half), (_address("kc", kc, u8, dev), _address("ks", ks, u8, dev, small), _address("vc", vc, u8, dev, shape),
+                                      _address("vs", vs, u8, dev, small))
 
 
 def polestar_k_kv4_append(k, v, idx, counts, kc, ks, vc, vs, k_scale=None, v_scale=None, k_deq=None, v_deq=None):
     """k, v [batch][R][n_kv*head_dim] into the cache rows idx [batch][R] (None: rows 0 .. R-1), of which counts [batch] are listed (None: R)."""
-    b, cap, n_kv, dh = _kv4_cache(kc, ks, vc, vs)
-    _need(k.dim() == 3, "k has to be [batch][R][n_kv*head_dim]")
-    R = k.shape[1]
-    for name, t in (("k", k), ("v", v)):
-        _buffer(name, t, k.dtype, (b, R, n_kv * dh))
-    for name, t in (("k_deq", k_deq), ("v_deq", v_deq)):
-        _buffer(name, t, k.dtype, k.shape, optional=True)
-    _buffer("idx", idx, torch.int32, (b, R), optional=True)
-    _buffer("counts", counts, torch.int32, (b,), optional=True)
-    for name, t in (("k_scale", k_scale), ("v_scale", v_scale)):
-        _buffer(name, t, torch.float32, (1,), optional=True)
-    _check(load().polestar_k_kv4_append(_ptr(k), _ptr(v), _ptr(idx), _ptr(counts), b, R, cap, n_kv, dh, _dtype_code(k), _ptr(k_scale),
-                                        _ptr(v_scale), _ptr(kc), _ptr(ks), _ptr(vc), _ptr(vs), _ptr(k_deq), _ptr(v_deq),
-                                        C.c_void_p(_stream())))
+    dev = _device("k", k)
+    if k.dim() != 3:
+        _refuse("k has to be [batch][R][n_kv*head_dim]")
+    (b, cap, n_kv, dh), cache = _kv4_cache(kc, ks, vc, vs, dev)
+    R, dt = k.shape[1], k.dtype
+    shape = (b, R, n_kv * dh)
+    _check(load().polestar_k_kv4_append(
+        _address("k", k, dt, dev, shape), _address("v", v, dt, dev, shape), _address("idx", idx, torch.int32, dev, (b, R), True),
+        _address("counts", counts, torch.int32, dev, (b,), True), b, R, cap, n_kv, dh, _dtype_code(k), _factor("k_scale", k_scale, dev),
+        _factor("v_scale", v_scale, dev), *cache, _address("k_deq", k_deq, dt, dev, shape, True), _address("v_deq", v_deq, dt, dev, shape, True),
+        _raw_stream(dev)))
 
 
 def polestar_k_kv4_scratch_bytes(batch, R, cap, n_heads, n_kv_heads, head_dim) -> int:
@@ -585,32 +615,32 @@ def polestar_k_kv4_scratch_bytes(batch, R, cap, n_heads, n_kv_heads, head_dim) -
 
 def polestar_k_kv4_attention(q, kc, ks, vc, vs, k_scale, v_scale, lens, out, lse, scratch):
     """q, out [batch][R][n_heads*head_dim], lse [batch][R][n_heads] (None: skipped), lens int32 [batch] (None: the whole cache)."""
-    b, cap, n_kv, dh = _kv4_cache(kc, ks, vc, vs)
-    _need(q.dim() == 3 and q.shape[2] % dh == 0, "q has to be [batch][R][n_heads*head_dim]")
-    R, n_heads = q.shape[1], q.shape[2] // dh
-    _buffer("q", q, q.dtype, (b, R, n_heads * dh))
-    _buffer("out", out, q.dtype, q.shape)
-    _buffer("lse", lse, torch.float32, (b, R, n_heads), optional=True)
-    _buffer("lens", lens, torch.int32, (b,), optional=True)
-    for name, t in (("k_scale", k_scale), ("v_scale", v_scale)):
-        _buffer(name, t, torch.float32, (1,), optional=True)
-    _buffer("scratch", scratch, torch.uint8)
-    _check(load().polestar_k_kv4_attention(_ptr(q), _ptr(kc), _ptr(ks), _ptr(vc), _ptr(vs), _ptr(k_scale), _ptr(v_scale), _ptr(lens), _ptr(out),
-                                           _ptr(lse), b, R, cap, n_heads, n_kv, dh, _dtype_code(q), _ptr(scratch), scratch.numel(),
-                                           C.c_void_p(_stream())))
+    dev = _device("q", q)
+    (b, cap, n_kv, dh), cache = _kv4_cache(kc, ks, vc, vs, dev)
+    if q.dim() != 3 or dh == 0 or q.shape[2] % dh:
+        _refuse("q has to be [batch][R][n_heads*head_dim]")
+    (qb, R, width), dt = q.shape, q.dtype
+    n_heads, shape = width // dh, (b, R, width)
+    _check(load().polestar_k_kv4_attention(
+        _address("q", q, dt, dev, shape), *cache, _factor("k_scale", k_scale, dev), _factor("v_scale", v_scale, dev),
+        _address("lens", lens, torch.int32, dev, (b,), True), _address("out", out, dt, dev, shape),
+        _address("lse", lse, torch.float32, dev, (b, R, n_heads), True), b, R, cap, n_heads, n_kv, dh, _dtype_code(q),
+        _address("scratch", scratch, torch.uint8, dev), scratch.numel(), _raw_stream(dev)))
 
 
 def polestar_k_token_logprobs(logits, target, mask_id, logprob, entropy, top_ids=None, top_logprobs=None):
     """logits [rows][vocab] (rows may be strided), target int32 [rows] -> logprob, entropy [rows], top_ids / top_logprobs [rows][k]."""
-    ld = _row_stride("logits", logits)
+    dev = _device("logits", logits)
+    ld = _row_stride("logits", logits, dev)
     rows, V = logits.shape
-    _buffer("target", target, torch.int32, (rows,), optional=logprob is None)
-    _buffer("logprob", logprob, torch.float32, (rows,), optional=True)
-    _buffer("entropy", entropy, torch.float32, (rows,), optional=True)
-    _need((top_ids is None) == (top_logprobs is None), "top_ids and top_logprobs come together")
-    _need(top_ids is None or top_ids.dim() == 2, "top_ids has to be [rows][k]")
+    if (top_ids is None) != (top_logprobs is None):
+        _refuse("top_ids and top_logprobs come together")
+    if top_ids is not None and top_ids.dim() != 2:
+        _refuse("top_ids has to be [rows][k]")
     k = 0 if top_ids is None else top_ids.shape[1]
-    _buffer("top_ids", top_ids, torch.int32, (rows, k), optional=True)
-    _buffer("top_logprobs", top_logprobs, torch.float32, (rows, k), optional=True)
-    _check(load().polestar_k_token_logprobs(_ptr(logits), ld, rows, V, _dtype_code(logits), _ptr(target), -1 if mask_id is None else mask_id, k,
-                                            _ptr(logprob), _ptr(entropy), _ptr(top_ids), _ptr(top_logprobs), C.c_void_p(_stream())))
+    f32, i32 = torch.float32, torch.int32
+    _check(load().polestar_k_token_logprobs(
+        logits.data_ptr(), ld, rows, V, _dtype_code(logits), _address("target", target, i32, dev, (rows,), logprob is None),
+        -1 if mask_id is None else mask_id, k, _address("logprob", logprob, f32, dev, (rows,), True),
+        _address("entropy", entropy, f32, dev, (rows,), True), _address("top_ids", top_ids, i32, dev, (rows, k), True),
+        _address("top_logprobs", top_logprobs, f32, dev, (rows, k), True), _raw_stream(dev)))
