@@ -52,26 +52,6 @@ static_assert(8 * 2 * PATCH_BYTES == (FL_MAX_SLOTS - FL_REC_SLOTS) * TILE_BYTES,
 constexpr float FL_SLACK = 8.f;           // log2 of how far the running maximum may lag behind
 __host__ __device__ constexpr size_t flash_smem_bytes(bool rec) { return (size_t)(rec ? 1 + FL_MAX_SLOTS : 2 + FL_PLAIN_SLOTS) * TILE_BYTES + 1024; }
 
-__device__ __forceinline__ void tmem_ld32_issue(uint32_t taddr, uint32_t* r) {
-    tmem_ld16_issue(taddr, r);
-    tmem_ld16_issue(taddr + 16, r + 16);
-}
-__device__ __forceinline__ void tmem_st16_issue(uint32_t taddr, const uint32_t* r) {
-    asm volatile(
-        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};"
-        ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
-          "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
-        : "memory");
-}
-// two fp32 values per instruction (rounded as the single operations are)
-__device__ __forceinline__ uint64_t f2_pack(float x, float y) { uint64_t r; asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(x), "f"(y)); return r; }
-__device__ __forceinline__ uint64_t f2_pack(uint32_t x, uint32_t y) { uint64_t r; asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "r"(x), "r"(y)); return r; }
-__device__ __forceinline__ void f2_unpack(uint64_t v, float& x, float& y) { asm("mov.b64 {%0, %1}, %2;" : "=f"(x), "=f"(y) : "l"(v)); }
-__device__ __forceinline__ uint64_t f2_fma(uint64_t a, uint64_t b, uint64_t c) { uint64_t r; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c)); return r; }
-__device__ __forceinline__ uint64_t f2_mul(uint64_t a, uint64_t b) { uint64_t r; asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
-__device__ __forceinline__ uint64_t f2_add(uint64_t a, uint64_t b) { uint64_t r; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
-__device__ __forceinline__ float f2_sum(uint64_t v) { float x, y; f2_unpack(v, x, y); return x + y; }
-__device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void bar_sync_streams() { asm volatile("bar.sync 1, 256;" ::: "memory"); }
 
 // A part of the forward's rows, the same of every sequence: `rows` of them, row r of the part being forward row r of the sequence,

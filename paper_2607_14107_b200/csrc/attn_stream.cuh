@@ -44,13 +44,6 @@ static_assert(COL_Q + DH / 2 <= TMEM_COLS, "tensor memory");
 
 __host__ __device__ constexpr size_t smem_bytes() { return (size_t)NS * TILE_BYTES + 2 * X_BYTES + 1024; }     // ring, X0, X1
 
-// A from tensor memory (lane = row, K-major, two bf16 per column), B from shared memory
-__device__ __forceinline__ void umma_bf16_ta(uint32_t tmem_d, uint32_t tmem_a, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
-    asm volatile(
-        "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}\n"
-        ::"r"(tmem_d), "r"(tmem_a), "l"(bdesc), "r"(idesc), "r"(accumulate)
-        : "memory");
-}
 // 16 columns of this thread's lane, complete on return (the whole warp calls)
 __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t* r) {
     asm volatile(

@@ -5,10 +5,12 @@
 // What a code and its scale stand for has six significant bits, so every key and value is exact in fp16 (and bf16); the tensors' factors are
 // applied to the scores and to the finished rows.  A row without keys is zero, its lse -inf.
 //
-// kv4_attn_warp_kernel (mma.sync m16n8k16, any type, head_dim 64 or 128): codes go from global memory to registers and become operand fragments
-// there, without passing through shared memory.  The order of channels inside a product is free, so a lane takes the fragments of keys from
-// consecutive channels of one row, and those of values from one group of 16 channels: its loads are 4 to 16 bytes, and a scale covers all
-// that it multiplies.  One pass with a running maximum that moves only when it has been outgrown by 2^8.
+// kv4_attn_warp_kernel (mma.sync m16n8k16, any type, head_dim 64 or 128): for few rows, where the stream of the cache and the instructions that
+// unpack it are the bound.  Sixteen keys are the 16 rows of the first operand (S^T = K Q^T) and sixteen channels of values are (O^T = V^T P^T), so
+// that 8 query rows fill a product.  A warp copies its own keys' codes into a ring of its own (cp.async, no barrier), and they become operand fragments
+// in registers: the order of channels inside a product is free, so a lane takes its fragments of keys from consecutive channels of a row and those of
+// values from one group of channels, and a scale covers all that it multiplies.  One pass with a running maximum that moves only when it has been
+// outgrown by 2^8.
 #pragma once
 #include <cuda_fp16.h>
 
@@ -17,10 +19,11 @@
 namespace ps {
 namespace kv4 {
 
-constexpr int ROWS = 16;                         // query rows of a CTA: rows of all heads that share a K/V head form one list, head-major
 constexpr int WARPS = 4, THREADS = WARPS * 32;
 constexpr int CHUNK = 16;                        // keys a warp takes at a time
+constexpr int DEPTH = 4;                         // chunks of a warp's ring
 constexpr int MAX_SPLIT = 64;
+constexpr int JOIN_THREADS = 64;
 constexpr float SLACK = 8.f;                     // log2 of how far the running maximum may lag behind
 constexpr float LIFT = 7.f;                      // probabilities are 2^(s - m + LIFT): fp16 then keeps them down to 2^-31 of the largest
 
@@ -31,6 +34,7 @@ struct Args {
     const int* lens;                             // [batch] keys of every sequence (null: cap)
     float* part_o; float2* part_ml;              // partial rows: [split][batch * R * n_heads][DH], (maximum, sum)
     int R, cap, n_heads, n_kv, split;
+    int part_keys;                               // keys of a part in the warp-level kernel
     long long rows_total;                        // batch * R * n_heads
     float scale;
 };
@@ -63,53 +67,6 @@ __device__ __forceinline__ uint32_t pack_half(float lo, float hi) {
 __device__ __forceinline__ float2 unpack_half(uint32_t w) { return __half22float2(*reinterpret_cast<const __half2*>(&w)); }
 
 __device__ __forceinline__ int seq_len(const Args& a, int b) { return a.lens ? min(max(__ldg(a.lens + b), 0), a.cap) : a.cap; }
-// keys [lo, hi) of part s of a sequence: whole chunks
-__device__ __forceinline__ void key_range(int len, int split, int s, int& lo, int& hi) {
-    const int chunks = (len + CHUNK - 1) / CHUNK;
-    lo = min(len, (int)((long long)chunks * s / split) * CHUNK);
-    hi = min(len, (int)((long long)chunks * (s + 1) / split) * CHUNK);
-}
-
-// the fragments' source words of one chunk
-template <int DH> struct Codes {
-    uint32_t k[2][DH / 32], ksc[2];              // two key rows: DH / 4 channels each, their scale bytes
-    uint32_t v[4][DH / 64], vsc[4];              // four value rows: DH / 8 channels each, the scale byte of their group
-};
-template <int N> __device__ __forceinline__ void load_words(const uint8_t* p, uint32_t (&w)[N]) {
-    if constexpr (N == 4) { const uint4 x = __ldg(reinterpret_cast<const uint4*>(p)); w[0] = x.x; w[1] = x.y; w[2] = x.z; w[3] = x.w; }
-    else if constexpr (N == 2) { const uint2 x = __ldg(reinterpret_cast<const uint2*>(p)); w[0] = x.x; w[1] = x.y; }
-    else w[0] = __ldg(reinterpret_cast<const uint32_t*>(p));
-}
-// Lane (g = lane / 4, t = lane % 4): keys g and g + 8, channels t DH/4 ..; values 2t, 2t + 1, 2t + 8, 2t + 9, channels g DH/8 ..
-// Rows from `hi` on are zeros (nothing is read there, whatever it holds).
-template <int DH>
-__device__ __forceinline__ void load_chunk(Codes<DH>& c, const Args& a, size_t row0, int j0, int hi, int g, int t, int kvh) {
-    const size_t stride_c = (size_t)a.n_kv * (DH / 2), stride_s = (size_t)a.n_kv * (DH / 16);
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        const int j = j0 + g + 8 * i;
-#pragma unroll
-        for (int w = 0; w < DH / 32; ++w) c.k[i][w] = 0u;
-        c.ksc[i] = 0u;
-        if (j < hi) {
-            load_words(a.kc + (row0 + j) * stride_c + kvh * (DH / 2) + t * (DH / 8), c.k[i]);
-            const uint8_t* s = a.ks + (row0 + j) * stride_s + kvh * (DH / 16) + t * (DH / 64);
-            c.ksc[i] = DH == 128 ? (uint32_t)__ldg(reinterpret_cast<const uint16_t*>(s)) : (uint32_t)__ldg(s) * 0x101u;
-        }
-    }
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int j = j0 + 2 * t + (i & 1) + 8 * (i >> 1);
-#pragma unroll
-        for (int w = 0; w < DH / 64; ++w) c.v[i][w] = 0u;
-        c.vsc[i] = 0u;
-        if (j < hi) {
-            load_words(a.vc + (row0 + j) * stride_c + kvh * (DH / 2) + g * (DH / 16), c.v[i]);
-            c.vsc[i] = __ldg(a.vs + (row0 + j) * stride_s + kvh * (DH / 16) + g * (DH / 8) / 16);
-        }
-    }
-}
-
 template <typename T> struct QPair;
 template <> struct QPair<float> { static __device__ __forceinline__ float2 load(const float* p) { return __ldg(reinterpret_cast<const float2*>(p)); } };
 template <> struct QPair<__nv_bfloat16> {
@@ -119,34 +76,89 @@ template <> struct QPair<__nv_bfloat16> {
     }
 };
 
-// grid: x = tile of rows x part of the keys, y = K/V head, z = sequence.
+// One warp's chunk in its ring: codes of 16 key rows and 16 value rows, their scales.
+template <int DH> struct Stage {
+    static constexpr uint32_t K = 0, V = CHUNK * DH / 2, KS = 2 * V, VS = KS + CHUNK * DH / 16, BYTES = VS + CHUNK * DH / 16;
+    // Byte offset of 16-byte piece p of a value row: with 128 channels, rows 2t and 2t + 1 share 128 bytes, and where a piece lies in them is such that
+    // the lanes' reads of one row parity spread over all banks.
+    static __device__ __forceinline__ uint32_t v_piece(int r, int p) {
+        if (DH == 64) return (uint32_t)(r * 32 + p * 16);
+        return (uint32_t)((r >> 1) * 128 + (((r ^ (r >> 2)) & 1) << 6) + ((p ^ (r & 2)) << 4));
+    }
+};
+template <int DH, int NB> __host__ __device__ constexpr size_t warp_smem_bytes() {
+    const size_t ring = (size_t)WARPS * DEPTH * Stage<DH>::BYTES, join = (size_t)WARPS * 8 * NB * (DH + 4) * 4;
+    return ring > join ? ring : join;
+}
+__device__ __forceinline__ uint32_t transpose8x8(uint32_t a) {
+    uint32_t d;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(a));
+    return d;
+}
+
+// grid: x = tile of 8 NB rows x part of the keys, y = K/V head, z = sequence.  Lane (g = lane / 4, t = lane % 4).
 // fp32 rows: q and the probabilities are each two fp16 terms (22 bits), with a product per term.
-template <typename T, int DH>
+template <typename T, int DH, int NB>
 __global__ void __launch_bounds__(THREADS) kv4_attn_warp_kernel(const __grid_constant__ Args a) {
     KERNEL_PROLOGUE(23);   // kv4_attn_warp_kernel
-    constexpr int TERMS = sizeof(T) == 4 ? 2 : 1, KS = DH / 16, NT = DH / 8;
-    __shared__ float so[WARPS][ROWS][DH + 4];
+    constexpr int TERMS = sizeof(T) == 4 ? 2 : 1, KS = DH / 16, MT = DH / 16, ROWS = 8 * NB;
+    using St = Stage<DH>;
+    extern __shared__ uint8_t smem_raw[];
     __shared__ float sm[WARPS][ROWS], sl[WARPS][ROWS];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
     const int tile = (int)blockIdx.x / a.split, part = (int)blockIdx.x - tile * a.split, kvh = blockIdx.y, b = blockIdx.z;
     const int hpg = a.n_heads / a.n_kv;
     const long long vrows = (long long)hpg * a.R, vr0 = (long long)tile * ROWS;
     const int len = seq_len(a, b);
-    int lo, hi;
-    key_range(len, a.split, part, lo, hi);
-    const size_t row0 = (size_t)b * a.cap;
+    const int lo = min(len, part * a.part_keys), hi = min(len, lo + a.part_keys);
     auto q_row = [&](long long vr) {             // virtual row -> row of [batch * R * n_heads]
         const int h = (int)(vr / a.R), r = (int)(vr - (long long)h * a.R);
         return ((size_t)b * a.R + r) * a.n_heads + kvh * hpg + h;
     };
+    if (lo >= hi && a.split > 1) {               // a part without keys: nothing but its empty sum
+        for (int i = threadIdx.x; i < ROWS; i += THREADS)
+            if (vr0 + i < vrows) a.part_ml[(size_t)part * a.rows_total + q_row(vr0 + i)] = make_float2(-INFINITY, 0.f);
+        return;
+    }
 
-    // q as operand fragments, every row scaled by a power of two to at most 2
-    uint32_t qf[TERMS][KS][4];
-    float unit[2];                               // of rows g and g + 8: scores in units of log 2
+    // ---- the ring: what this lane copies of a chunk (sixteen-byte pieces of codes, the scales of one row) ----
+    constexpr int PIECES = DH / 32, COPIES = CHUNK * PIECES / 32;          // of a row; per lane, keys and values each
+    const uint32_t ring = (uint32_t)__cvta_generic_to_shared(smem_raw) + (uint32_t)warp * (DEPTH * St::BYTES);
+    const size_t row_c = (size_t)a.n_kv * (DH / 2), row_s = (size_t)a.n_kv * (DH / 16), seq0 = (size_t)b * a.cap;
+    int fj = lo + warp * CHUNK;                                            // first key of the next chunk to fetch
+    const uint8_t* fk = a.kc + (seq0 + fj) * row_c + kvh * (DH / 2);
+    const uint8_t* fv = a.vc + (seq0 + fj) * row_c + kvh * (DH / 2);
+    const uint8_t* fs = (lane < 16 ? a.ks : a.vs) + (seq0 + fj + (lane & 15)) * row_s + kvh * (DH / 16);
+    auto fetch = [&](int slot) {
+        const uint32_t dst = ring + (uint32_t)slot * St::BYTES;
+        if (fj < hi) {
+#pragma unroll
+            for (int i = 0; i < COPIES; ++i) {
+                const int x = i * 32 + lane, r = x / PIECES, p = x % PIECES;
+                const uint32_t n = fj + r < hi ? 16u : 0u;                 // rows from the end on are zeros and not read
+                const size_t off = n ? (size_t)r * row_c + p * 16 : 0;
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst + St::K + (uint32_t)(x * 16)), "l"(fk + off), "r"(n) : "memory");
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst + St::V + St::v_piece(r, p)), "l"(fv + off), "r"(n) : "memory");
+            }
+            const bool in = fj + (lane & 15) < hi;
+            const uint8_t* src = in ? fs : a.ks;
+            if constexpr (DH == 128) asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"(dst + St::KS + (uint32_t)lane * 8u), "l"(src), "r"(in ? 8u : 0u) : "memory");
+            else asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst + St::KS + (uint32_t)lane * 4u), "l"(src), "r"(in ? 4u : 0u) : "memory");
+            fj += WARPS * CHUNK;
+            fk += WARPS * CHUNK * row_c; fv += WARPS * CHUNK * row_c; fs += WARPS * CHUNK * row_s;
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+#pragma unroll
+    for (int i = 0; i < DEPTH - 1; ++i) fetch(i);
+
+    // ---- q as operand fragments, every row scaled by a power of two to at most 2: row g, channels t DH/4 .. ----
+    uint32_t qf[TERMS][NB][KS][2];
+    float unit[NB][2];                           // of rows 2t, 2t + 1: scores in units of log 2
     const float tk = a.tk ? __ldg(a.tk) : 1.f;
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        const long long vr = vr0 + g + 8 * i;
+    for (int n = 0; n < NB; ++n) {
+        const long long vr = vr0 + 8 * n + g;
         const T* q = (const T*)a.q + (vr < vrows ? q_row(vr) : 0) * DH + t * (DH / 4);
         float2 x[DH / 8];
         uint32_t top = 0;
@@ -159,131 +171,179 @@ __global__ void __launch_bounds__(THREADS) kv4_attn_warp_kernel(const __grid_con
         top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
         const int e = min(max((int)(top >> 23), 1), 253);          // biased exponent of the largest magnitude
         const float down = __uint_as_float((uint32_t)(254 - e) << 23), up = __uint_as_float((uint32_t)e << 23);
-        unit[i] = up * (a.scale * 1.4426950408889634f * tk);
+        const float un = up * (a.scale * 1.4426950408889634f * tk);
+        unit[n][0] = __shfl_sync(0xffffffffu, un, 8 * t);
+        unit[n][1] = __shfl_sync(0xffffffffu, un, 8 * t + 4);
 #pragma unroll
         for (int s = 0; s < KS; ++s)
 #pragma unroll
             for (int p = 0; p < 2; ++p) {
                 const float2 v = make_float2(x[2 * s + p].x * down, x[2 * s + p].y * down);
                 const uint32_t w = pack_half(v.x, v.y);
-                qf[0][s][2 * p + i] = w;
+                qf[0][n][s][p] = w;
                 if (TERMS == 2) {
                     const float2 r = unpack_half(w);
-                    qf[TERMS - 1][s][2 * p + i] = pack_half(v.x - r.x, v.y - r.y);
+                    qf[TERMS - 1][n][s][p] = pack_half(v.x - r.x, v.y - r.y);
                 }
             }
     }
 
-    float o[NT][4];
+    float o[MT][NB][4];                          // channel g DH/8 + 2 mt + (x >> 1), row 2t + (x & 1)
 #pragma unroll
-    for (int n = 0; n < NT; ++n) { o[n][0] = o[n][1] = o[n][2] = o[n][3] = 0.f; }
-    float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};       // l: this lane's columns only
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int n = 0; n < NB; ++n) o[i][n][0] = o[i][n][1] = o[i][n][2] = o[i][n][3] = 0.f;
+    float m[NB][2], l[NB][2];                    // l: this lane's keys only
+#pragma unroll
+    for (int n = 0; n < NB; ++n) { m[n][0] = m[n][1] = -INFINITY; l[n][0] = l[n][1] = 0.f; }
 
-    Codes<DH> cur, nxt;
-    int j0 = lo + warp * CHUNK;
-    if (j0 < hi) load_chunk<DH>(cur, a, row0, j0, hi, g, t, kvh);
-    for (; j0 < hi; j0 += WARPS * CHUNK) {
-        const int jn = j0 + WARPS * CHUNK;
-        if (jn < hi) load_chunk<DH>(nxt, a, row0, jn, hi, g, t, kvh);
-        float s[2][4];
+    int slot = 0;
+    for (int j0 = lo + warp * CHUNK; j0 < hi; j0 += WARPS * CHUNK) {
+        asm volatile("cp.async.wait_group %0;" ::"n"(DEPTH - 2) : "memory");
+        __syncwarp();                            // the chunk has landed for every lane, and everybody is done with the slot in front of it
+        fetch(slot == 0 ? DEPTH - 1 : slot - 1);
+        const uint32_t st = ring + (uint32_t)slot * St::BYTES;
+        slot = slot + 1 == DEPTH ? 0 : slot + 1;
+        // scores of keys g and g + 8 (rows of the product) against rows 2t, 2t + 1
+        float s[NB][4];
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            s[i][0] = s[i][1] = s[i][2] = s[i][3] = 0.f;
-            const uint32_t sp = scales_to_half(cur.ksc[i]);
-            const uint32_t s0 = __byte_perm(sp, 0, 0x1010), s1 = __byte_perm(sp, 0, 0x3232);
+        for (int n = 0; n < NB; ++n) s[n][0] = s[n][1] = s[n][2] = s[n][3] = 0.f;
+        {
+            uint32_t kw[2][DH / 32], ksc[2];
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const uint32_t row = (uint32_t)(g + 8 * i);
+                if constexpr (DH == 128) {
+                    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(kw[i][0]), "=r"(kw[i][1]), "=r"(kw[i][2]), "=r"(kw[i][3]) : "r"(st + St::K + row * 64u + (uint32_t)t * 16u) : "memory");
+                    asm volatile("{\n .reg .u16 h;\n ld.shared.u16 h, [%1];\n cvt.u32.u16 %0, h;\n}\n" : "=r"(ksc[i]) : "r"(st + St::KS + row * 8u + (uint32_t)t * 2u) : "memory");
+                } else {
+                    asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(kw[i][0]), "=r"(kw[i][1]) : "r"(st + St::K + row * 32u + (uint32_t)t * 8u) : "memory");
+                    asm volatile("{\n .reg .u16 h;\n ld.shared.u8 h, [%1];\n cvt.u32.u16 %0, h;\n}\n" : "=r"(ksc[i]) : "r"(st + St::KS + row * 4u + (uint32_t)t) : "memory");
+                    ksc[i] *= 0x101u;
+                }
+            }
+            const uint32_t sp0 = scales_to_half(ksc[0]), sp1 = scales_to_half(ksc[1]);
 #pragma unroll
             for (int w = 0; w < DH / 32; ++w) {
-                uint32_t h[4];
-                codes_to_half(cur.k[i][w], h);
-                const uint32_t sc = w < DH / 64 ? s0 : s1;
+                const uint32_t sel = w < DH / 64 ? 0x1010u : 0x3232u;
+                const uint32_t sc0 = __byte_perm(sp0, 0, sel), sc1 = __byte_perm(sp1, 0, sel);
+                uint32_t h0[4], h1[4];
+                codes_to_half(kw[0][w], h0);
+                codes_to_half(kw[1][w], h1);
 #pragma unroll
-                for (int x = 0; x < 4; ++x) h[x] = h2mul(h[x], sc);
+                for (int x = 0; x < 4; ++x) { h0[x] = h2mul(h0[x], sc0); h1[x] = h2mul(h1[x], sc1); }
 #pragma unroll
-                for (int tm = 0; tm < TERMS; ++tm) {
-                    mma16816(s[i], qf[tm][2 * w], h[0], h[1]);
-                    mma16816(s[i], qf[tm][2 * w + 1], h[2], h[3]);
+                for (int y = 0; y < 2; ++y) {
+                    const uint32_t fa[4] = {h0[2 * y], h1[2 * y], h0[2 * y + 1], h1[2 * y + 1]};
+#pragma unroll
+                    for (int n = 0; n < NB; ++n)
+#pragma unroll
+                        for (int tm = 0; tm < TERMS; ++tm) mma16816(s[n], fa, qf[tm][n][2 * w + y][0], qf[tm][n][2 * w + y][1]);
                 }
             }
         }
-        // columns of s[i]: keys j0 + 8 i + 2 t, + 1; [0], [1]: row g, [2], [3]: row g + 8
-        float top[2];
+        bool grow = false;
+        float top[NB][2];
 #pragma unroll
-        for (int r = 0; r < 2; ++r) {
-            top[r] = -INFINITY;
+        for (int n = 0; n < NB; ++n) {
 #pragma unroll
-            for (int i = 0; i < 2; ++i)
+            for (int x = 0; x < 4; ++x) s[n][x] *= unit[n][x & 1];
+            if (__builtin_expect(j0 + CHUNK > hi, 0)) {
+                if (j0 + g >= hi) s[n][0] = s[n][1] = -INFINITY;
+                if (j0 + g + 8 >= hi) s[n][2] = s[n][3] = -INFINITY;
+            }
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+                top[n][x] = fmaxf(s[n][x], s[n][x + 2]);
+                grow |= top[n][x] > m[n][x] + SLACK;
+            }
+        }
+        if (__any_sync(0xffffffffu, grow)) {
+#pragma unroll
+            for (int n = 0; n < NB; ++n)
 #pragma unroll
                 for (int x = 0; x < 2; ++x) {
-                    float& v = s[i][2 * r + x];
-                    v = j0 + 8 * i + 2 * t + x < hi ? v * unit[r] : -INFINITY;
-                    top[r] = fmaxf(top[r], v);
+                    float nm = top[n][x];
+#pragma unroll
+                    for (int d = 4; d < 32; d <<= 1) nm = fmaxf(nm, __shfl_xor_sync(0xffffffffu, nm, d));
+                    nm = nm > m[n][x] + SLACK ? nm : m[n][x];
+                    const float f = m[n][x] == -INFINITY ? 0.f : ex2(m[n][x] - nm);
+                    m[n][x] = nm;
+                    l[n][x] *= f;
+#pragma unroll
+                    for (int i = 0; i < MT; ++i) { o[i][n][x] *= f; o[i][n][x + 2] *= f; }
                 }
         }
-        if (__any_sync(0xffffffffu, top[0] > m[0] + SLACK || top[1] > m[1] + SLACK)) {
+        uint32_t pf[TERMS][NB][2];
 #pragma unroll
-            for (int r = 0; r < 2; ++r) {
-                float nm = fmaxf(top[r], __shfl_xor_sync(0xffffffffu, top[r], 1));
-                nm = fmaxf(nm, __shfl_xor_sync(0xffffffffu, nm, 2));
-                nm = nm > m[r] + SLACK ? nm : m[r];
-                const float f = m[r] == -INFINITY ? 0.f : ex2(m[r] - nm);
-                m[r] = nm;
-                l[r] *= f;
+        for (int n = 0; n < NB; ++n) {
+            float p[4];
 #pragma unroll
-                for (int n = 0; n < NT; ++n) { o[n][2 * r] *= f; o[n][2 * r + 1] *= f; }
+            for (int x = 0; x < 4; ++x) {
+                const float base = m[n][x & 1] == -INFINITY ? 0.f : m[n][x & 1] - LIFT;      // (nothing but -inf so far: p = 0)
+                p[x] = ex2(s[n][x] - base);
             }
-        }
-        uint32_t pf[TERMS][4];
-#pragma unroll
-        for (int i = 0; i < 2; ++i)
-#pragma unroll
-            for (int r = 0; r < 2; ++r) {
-                const float base = m[r] == -INFINITY ? 0.f : m[r] - LIFT;      // (nothing but -inf so far: p = 0)
-                const float p0 = ex2(s[i][2 * r] - base), p1 = ex2(s[i][2 * r + 1] - base);
-                l[r] += p0 + p1;
-                const uint32_t w = pack_half(p0, p1);
-                pf[0][2 * i + r] = w;
-                if (TERMS == 2) {
-                    const float2 back = unpack_half(w);
-                    pf[TERMS - 1][2 * i + r] = pack_half(p0 - back.x, p1 - back.y);
-                }
-            }
-        // values: nibbles of two neighbouring rows side by side, so that one conversion gives a fragment register
-        const uint32_t vs0 = scales_to_half(cur.vsc[0] | (cur.vsc[1] << 8)), vs1 = scales_to_half(cur.vsc[2] | (cur.vsc[3] << 8));
-#pragma unroll
-        for (int w = 0; w < DH / 64; ++w) {
-            uint32_t b0[8], b1[8];
+            l[n][0] += p[0] + p[2];
+            l[n][1] += p[1] + p[3];
 #pragma unroll
             for (int y = 0; y < 2; ++y) {
-                const uint32_t r0 = cur.v[2 * y][w], r1 = cur.v[2 * y + 1][w];
-                const uint32_t even = (r0 & 0x0f0f0f0fu) | ((r1 << 4) & 0xf0f0f0f0u), odd = ((r0 >> 4) & 0x0f0f0f0fu) | (r1 & 0xf0f0f0f0u);
-                uint32_t he[4], ho[4];
-                codes_to_half(even, he);
-                codes_to_half(odd, ho);
-#pragma unroll
-                for (int x = 0; x < 4; ++x) {
-                    (y ? b1 : b0)[2 * x] = h2mul(he[x], y ? vs1 : vs0);
-                    (y ? b1 : b0)[2 * x + 1] = h2mul(ho[x], y ? vs1 : vs0);
+                const uint32_t w = pack_half(p[2 * y], p[2 * y + 1]);
+                pf[0][n][y] = transpose8x8(w);   // keys g (+ 8), rows 2t.. -> keys 2t.. (+ 8), row g
+                if (TERMS == 2) {
+                    const float2 back = unpack_half(w);
+                    pf[TERMS - 1][n][y] = transpose8x8(pack_half(p[2 * y] - back.x, p[2 * y + 1] - back.y));
                 }
             }
-#pragma unroll
-            for (int x = 0; x < 8; ++x)
-#pragma unroll
-                for (int tm = 0; tm < TERMS; ++tm) mma16816(o[8 * w + x], pf[tm], b0[x], b1[x]);
         }
-        cur = nxt;
+        // values 2t, 2t + 1, 2t + 8, 2t + 9, channels g DH/8 ..: nibbles of two neighbouring rows side by side, so that one conversion gives a register
+        uint32_t vw[4][DH / 64], vsc[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int row = 2 * t + (i & 1) + 8 * (i >> 1);
+            if constexpr (DH == 128) {
+                asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(vw[i][0]), "=r"(vw[i][1]) : "r"(st + St::V + St::v_piece(row, g >> 1) + (uint32_t)(g & 1) * 8u) : "memory");
+                asm volatile("{\n .reg .u16 h;\n ld.shared.u8 h, [%1];\n cvt.u32.u16 %0, h;\n}\n" : "=r"(vsc[i]) : "r"(st + St::VS + (uint32_t)(row * 8 + g)) : "memory");
+            } else {
+                asm volatile("ld.shared.b32 %0, [%1];" : "=r"(vw[i][0]) : "r"(st + St::V + (uint32_t)(row * 32 + g * 4)) : "memory");
+                asm volatile("{\n .reg .u16 h;\n ld.shared.u8 h, [%1];\n cvt.u32.u16 %0, h;\n}\n" : "=r"(vsc[i]) : "r"(st + St::VS + (uint32_t)(row * 4 + (g >> 1))) : "memory");
+            }
+        }
+        const uint32_t vs0 = scales_to_half(vsc[0] | (vsc[1] << 8)), vs1 = scales_to_half(vsc[2] | (vsc[3] << 8));
+#pragma unroll
+        for (int w = 0; w < DH / 64; ++w) {
+            uint32_t he[2][4], ho[2][4];         // even and odd channels, keys 2t.. and 2t + 8 ..
+#pragma unroll
+            for (int y = 0; y < 2; ++y) {
+                const uint32_t r0 = vw[2 * y][w], r1 = vw[2 * y + 1][w];
+                codes_to_half((r0 & 0x0f0f0f0fu) | ((r1 << 4) & 0xf0f0f0f0u), he[y]);
+                codes_to_half(((r0 >> 4) & 0x0f0f0f0fu) | (r1 & 0xf0f0f0f0u), ho[y]);
+            }
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+                const uint32_t fa[4] = {h2mul(he[0][x], vs0), h2mul(ho[0][x], vs0), h2mul(he[1][x], vs1), h2mul(ho[1][x], vs1)};
+#pragma unroll
+                for (int n = 0; n < NB; ++n)
+#pragma unroll
+                    for (int tm = 0; tm < TERMS; ++tm) mma16816(o[4 * w + x][n], fa, pf[tm][n][0], pf[tm][n][1]);
+            }
+        }
     }
 
-    // ---- the warps' parts of the rows together: tile n's column c is channel c DH/8 + n ----
+    // ---- the warps' parts of the rows together, in the ring's place ----
+    asm volatile("cp.async.wait_all;" ::: "memory");
+    __syncthreads();
+    float (*so)[ROWS][DH + 4] = reinterpret_cast<float (*)[ROWS][DH + 4]>(smem_raw);
 #pragma unroll
-    for (int r = 0; r < 2; ++r) {
-        l[r] += __shfl_xor_sync(0xffffffffu, l[r], 1);
-        l[r] += __shfl_xor_sync(0xffffffffu, l[r], 2);
-        if (t == 0) { sm[warp][g + 8 * r] = m[r]; sl[warp][g + 8 * r] = l[r]; }
-    }
+    for (int n = 0; n < NB; ++n)
 #pragma unroll
-    for (int n = 0; n < NT; ++n)
+        for (int x = 0; x < 2; ++x) {
 #pragma unroll
-        for (int x = 0; x < 4; ++x) so[warp][g + 8 * (x >> 1)][(2 * t + (x & 1)) * (DH / 8) + n] = o[n][x];
+            for (int d = 4; d < 32; d <<= 1) l[n][x] += __shfl_xor_sync(0xffffffffu, l[n][x], d);
+            if (g == 0) { sm[warp][8 * n + 2 * t + x] = m[n][x]; sl[warp][8 * n + 2 * t + x] = l[n][x]; }
+#pragma unroll
+            for (int i = 0; i < MT; ++i)
+                *reinterpret_cast<float2*>(&so[warp][8 * n + 2 * t + x][g * (DH / 8) + 2 * i]) = make_float2(o[i][n][x], o[i][n][x + 2]);
+        }
     __syncthreads();
     const float tv = a.tv ? __ldg(a.tv) : 1.f;
     for (int i = threadIdx.x; i < ROWS * (DH / 4); i += THREADS) {
@@ -297,7 +357,7 @@ __global__ void __launch_bounds__(THREADS) kv4_attn_warp_kernel(const __grid_con
         float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
         for (int w = 0; w < WARPS; ++w) {
-            const float f = sm[w][r] == -INFINITY ? (sl[w][r] == 0.f ? 0.f : 1.f) : ex2(sm[w][r] - mm);
+            const float f = sm[w][r] == -INFINITY ? (sl[w][r] == 0.f ? 0.f : 1.f) : ex2(sm[w][r] - mm);      // (nothing but NaN scores: m = -inf, l = NaN)
             const float4 x = *reinterpret_cast<const float4*>(&so[w][r][c]);
             ll += f * sl[w][r];
             acc.x += f * x.x; acc.y += f * x.y; acc.z += f * x.z; acc.w += f * x.w;
@@ -319,11 +379,11 @@ __global__ void __launch_bounds__(THREADS) kv4_attn_warp_kernel(const __grid_con
 
 // The parts of the rows put together in their order; a warp per row.
 template <typename T, int DH>
-__global__ void __launch_bounds__(256) kv4_attn_join_kernel(const __grid_constant__ Args a) {
+__global__ void __launch_bounds__(JOIN_THREADS) kv4_attn_join_kernel(const __grid_constant__ Args a) {
     KERNEL_PROLOGUE(24);   // kv4_attn_join_kernel
     constexpr int PER = DH / 32;
     const int lane = threadIdx.x & 31;
-    const long long row = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
+    const long long row = (long long)blockIdx.x * (JOIN_THREADS / 32) + (threadIdx.x >> 5);
     if (row >= a.rows_total) return;
     float2 ml[MAX_SPLIT / 32];
     float mm = -INFINITY;
@@ -344,14 +404,21 @@ __global__ void __launch_bounds__(256) kv4_attn_join_kernel(const __grid_constan
     float acc[PER];
 #pragma unroll
     for (int c = 0; c < PER; ++c) acc[c] = 0.f;
-    for (int p = 0; p < a.split; ++p) {
-        const float f = __shfl_sync(0xffffffffu, p < 32 ? ml[0].x : ml[MAX_SPLIT / 32 - 1].x, p & 31);
-        const float* src = a.part_o + ((size_t)p * a.rows_total + row) * DH + lane * PER;
+    for (int p0 = 0; p0 < a.split; p0 += 8) {    // eight parts' loads in flight
+        float f[8];
+        float2 x[8][PER / 2];
 #pragma unroll
-        for (int c = 0; c < PER; c += 2) {
-            const float2 x = __ldcg(reinterpret_cast<const float2*>(src + c));
-            acc[c] += f * x.x; acc[c + 1] += f * x.y;
+        for (int i = 0; i < 8; ++i) {
+            const int p = p0 + i;                // (behind the last part: a weight of 0, as an empty part has, which has written no row)
+            f[i] = __shfl_sync(0xffffffffu, p < 32 ? ml[0].x : ml[MAX_SPLIT / 32 - 1].x, p & 31);
+            const float* src = a.part_o + ((size_t)p * a.rows_total + row) * DH + lane * PER;
+#pragma unroll
+            for (int c = 0; c < PER / 2; ++c) x[i][c] = f[i] != 0.f ? __ldcg(reinterpret_cast<const float2*>(src) + c) : make_float2(0.f, 0.f);
         }
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+#pragma unroll
+            for (int c = 0; c < PER / 2; ++c) { acc[2 * c] += f[i] * x[i][c].x; acc[2 * c + 1] += f[i] * x[i][c].y; }
     }
     const float tv = a.tv ? __ldg(a.tv) : 1.f, inv = ll == 0.f ? 0.f : tv / ll;
     T* out = (T*)a.out + (size_t)row * DH + lane * PER;

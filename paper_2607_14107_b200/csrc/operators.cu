@@ -9,16 +9,26 @@
 #include <atomic>
 #include <climits>
 #include <cmath>
+#include <cstdlib>
 #include <mutex>
 
 #include "fp4.cuh"
 #include "fp4_gemm.cuh"
-#include "kv4_attn.cuh"
+#include "kv4_attn_tc.cuh"
 #include "logprobs.cuh"
 
 using namespace ps;
 
 #define CK(call) do { if ((call) != cudaSuccess) return POLESTAR_E_CUDA; } while (0)
+
+// Environment switches: read by the first call and by polestar_reload_env, never on the launch path.
+//   POLESTAR_KV4_KERNEL (0 = automatic): 1 the warp-level attention kernel, 2 the tensor-core one where it applies (used by the tests)
+static std::atomic<int> g_kv4_kernel{-1};
+namespace ps { void reload_operator_switches() { const char* e = getenv("POLESTAR_KV4_KERNEL"); g_kv4_kernel.store(e ? atoi(e) : 0); } }
+static int switch_kv4() {
+    if (g_kv4_kernel.load() < 0) reload_operator_switches();
+    return g_kv4_kernel.load();
+}
 
 // Facts of the CURRENT device; the first call on a device queries them and raises the shared-memory limits of the kernels that need
 // more than the default there (function attributes are per device).
@@ -196,12 +206,43 @@ extern "C" int polestar_k_kv4_append(const void* k, const void* v, const int32_t
     return POLESTAR_OK;
 }
 
-// Parts that the keys are split into: enough CTAs for three on every SM of a B200, no part shorter than four chunks a warp.  A function of the
-// sizes alone, so that a scratch of polestar_k_kv4_scratch_bytes() bytes suffices for every call of these sizes.
-static int kv4_split(long long batch, long long R, int cap, int n_heads, int n_kv) {
-    const long long tiles = (R * (n_heads / n_kv) + kv4::ROWS - 1) / kv4::ROWS, base = batch * n_kv * tiles;
-    const long long most = std::max<long long>(1, cap / (4 * kv4::CHUNK * kv4::WARPS));
-    return (int)std::max<long long>(1, std::min<long long>(std::min<long long>(kv4::MAX_SPLIT, most), 3 * 148 / std::max<long long>(base, 1)));
+// Plans of the attention kernels: functions of the sizes alone, so that a scratch of polestar_k_kv4_scratch_bytes() bytes suffices for every call of
+// these sizes.  The warp-level kernel: tiles of 8 or 16 rows, parts of a fixed number of keys (those behind a short sequence's end leave at once).
+struct Kv4Warp { int tiles, rows, part_keys, split; };
+static Kv4Warp kv4_warp_plan(long long batch, long long R, int cap, int n_heads, int n_kv) {
+    const long long vrows = R * (n_heads / n_kv);
+    Kv4Warp p;
+    p.rows = vrows <= 8 ? 8 : 16;
+    p.tiles = (int)((vrows + p.rows - 1) / p.rows);
+    const int step = kv4::CHUNK * kv4::WARPS;
+    const long long base = std::max<long long>(1, batch * n_kv * p.tiles);
+    const long long want = std::max<long long>(1, std::min<long long>(kv4::MAX_SPLIT, 6 * 148 / base));
+    p.part_keys = std::max<int>(512, (int)((cap + want - 1) / want));
+    p.part_keys = (p.part_keys + step - 1) / step * step;
+    p.split = (cap + p.part_keys - 1) / p.part_keys;
+    return p;
+}
+// The same for the tensor-core kernel: row tiles of 128 (one of them: split between the streams of a CTA) or pairs of them, one CTA per SM.  The
+// number of parts that needs the fewest waves of key tiles, a part being no shorter than four tiles.
+struct Kv4Tc { int tiles, key_split, split; };
+static Kv4Tc kv4_tc_plan(long long batch, long long R, int cap, int n_heads, int n_kv) {
+    const long long row_tiles = (R * (n_heads / n_kv) + kv4::TC_ROWS - 1) / kv4::TC_ROWS;
+    Kv4Tc p;
+    p.key_split = row_tiles == 1;
+    p.tiles = (int)((row_tiles + 1) / 2);
+    const long long base = batch * n_kv * p.tiles, key_tiles = (cap + kv4::TC_KEYS - 1) / kv4::TC_KEYS;
+    p.split = 1;
+    double best = 1e30;
+    for (int s = 1; s <= kv4::MAX_SPLIT && (s == 1 || key_tiles / s >= 4); ++s) {
+        const double cost = (double)((base * s + 147) / 148) * (double)((key_tiles + s - 1) / s + 2);       // two tiles' worth of start and end
+        if (cost < 0.97 * best) { best = cost; p.split = s; }
+    }
+    return p;
+}
+static bool kv4_use_tc(int dtype, int head_dim, long long vrows) {
+    if (dtype != POLESTAR_BF16 || head_dim != kv4::TC_DH) return false;
+    const int forced = switch_kv4();
+    return forced ? forced == 2 : vrows > 16;
 }
 static bool kv4_attention_shape_ok(int batch, int R, int cap, int n_heads, int n_kv, int head_dim) {
     return kv4_shape_ok(batch, R, cap, n_kv, head_dim) && R <= 65536 && n_heads > 0 && n_heads <= 1024 && n_heads % n_kv == 0;
@@ -210,17 +251,30 @@ static bool kv4_attention_shape_ok(int batch, int R, int cap, int n_heads, int n
 extern "C" size_t polestar_k_kv4_scratch_bytes(int32_t batch, int32_t R, int32_t cap, int32_t n_heads, int32_t n_kv, int32_t head_dim) {
     if (!kv4_attention_shape_ok(batch, R, cap, n_heads, n_kv, head_dim)) return 0;
     const size_t rows = (size_t)batch * R * n_heads;
-    const int split = kv4_split(batch, R, cap, n_heads, n_kv);
+    const int split = std::max(kv4_warp_plan(batch, R, cap, n_heads, n_kv).split, kv4_tc_plan(batch, R, cap, n_heads, n_kv).split);
     return 256 + (split > 1 ? split * rows * ((size_t)head_dim * 4 + 8) : 0);
 }
 
-template <typename T, int DH>
-static int launch_kv4_warp(const kv4::Args& a, int batch, cudaStream_t st) {
-    const long long tiles = ((long long)a.R * (a.n_heads / a.n_kv) + kv4::ROWS - 1) / kv4::ROWS;
-    if (tiles * a.split > INT32_MAX) return POLESTAR_E_INVAL;
-    CK(launch_k(kv4::kv4_attn_warp_kernel<T, DH>, dim3((unsigned)(tiles * a.split), a.n_kv, batch), dim3(kv4::THREADS), 0, st, a));
-    if (a.split > 1) CK(launch_k(kv4::kv4_attn_join_kernel<T, DH>, dim3((unsigned)((a.rows_total + 7) / 8)), dim3(256), 0, st, a));
+static dim3 join_grid(const kv4::Args& a) { return dim3((unsigned)((a.rows_total * 32 + kv4::JOIN_THREADS - 1) / kv4::JOIN_THREADS)); }
+static int launch_kv4_tc(const kv4::Args& a, const Kv4Tc& p, int batch, cudaStream_t st) {
+    kv4::TcArgs f;
+    f.a = a; f.tiles = p.tiles; f.key_split = p.key_split;
+    if ((long long)p.tiles * a.split > INT32_MAX) return POLESTAR_E_INVAL;
+    CK(launch_k(kv4::kv4_attn_tc_kernel, dim3((unsigned)(p.tiles * a.split), a.n_kv, batch), dim3(kv4::TC_THREADS), kv4::TC_SMEM, st, f));
+    if (a.split > 1) CK(launch_k(kv4::kv4_attn_join_kernel<__nv_bfloat16, 128>, join_grid(a), dim3(kv4::JOIN_THREADS), 0, st, a));
     return POLESTAR_OK;
+}
+template <typename T, int DH, int NB>
+static int launch_kv4_warp(const kv4::Args& a, const Kv4Warp& p, int batch, cudaStream_t st) {
+    if ((long long)p.tiles * p.split > INT32_MAX) return POLESTAR_E_INVAL;
+    CK(launch_k(kv4::kv4_attn_warp_kernel<T, DH, NB>, dim3((unsigned)(p.tiles * p.split), a.n_kv, batch), dim3(kv4::THREADS), kv4::warp_smem_bytes<DH, NB>(), st, a));
+    if (a.split > 1) CK(launch_k(kv4::kv4_attn_join_kernel<T, DH>, join_grid(a), dim3(kv4::JOIN_THREADS), 0, st, a));
+    return POLESTAR_OK;
+}
+template <typename T>
+static int launch_kv4_warp(const kv4::Args& a, const Kv4Warp& p, int head_dim, int batch, cudaStream_t st) {
+    if (head_dim == 128) return p.rows == 8 ? launch_kv4_warp<T, 128, 1>(a, p, batch, st) : launch_kv4_warp<T, 128, 2>(a, p, batch, st);
+    return p.rows == 8 ? launch_kv4_warp<T, 64, 1>(a, p, batch, st) : launch_kv4_warp<T, 64, 2>(a, p, batch, st);
 }
 
 extern "C" int polestar_k_kv4_attention(const void* q, const uint8_t* kc, const uint8_t* ks, const uint8_t* vc, const uint8_t* vs,
@@ -240,13 +294,18 @@ extern "C" int polestar_k_kv4_attention(const void* q, const uint8_t* kc, const 
     kv4::Args a;
     a.q = q; a.out = out; a.lse = lse; a.kc = kc; a.ks = ks; a.vc = vc; a.vs = vs; a.tk = k_scale; a.tv = v_scale; a.lens = lens;
     a.R = R; a.cap = cap; a.n_heads = n_heads; a.n_kv = n_kv; a.rows_total = (long long)batch * R * n_heads;
-    a.split = kv4_split(batch, R, cap, n_heads, n_kv);
+    const bool tc = kv4_use_tc(dtype, head_dim, (long long)R * (n_heads / n_kv));
+    const Kv4Tc plan = kv4_tc_plan(batch, R, cap, n_heads, n_kv);
+    const Kv4Warp wplan = kv4_warp_plan(batch, R, cap, n_heads, n_kv);
+    a.split = tc ? plan.split : wplan.split;
+    a.part_keys = wplan.part_keys;
     a.part_o = (float*)scratch;
     a.part_ml = (float2*)((char*)scratch + (size_t)a.split * a.rows_total * head_dim * 4);
     a.scale = 1.0f / sqrtf((float)head_dim);
     cudaStream_t st = (cudaStream_t)stream;
-    if (dtype == POLESTAR_BF16) return head_dim == 128 ? launch_kv4_warp<__nv_bfloat16, 128>(a, batch, st) : launch_kv4_warp<__nv_bfloat16, 64>(a, batch, st);
-    return head_dim == 128 ? launch_kv4_warp<float, 128>(a, batch, st) : launch_kv4_warp<float, 64>(a, batch, st);
+    if (tc) return launch_kv4_tc(a, plan, batch, st);
+    if (dtype == POLESTAR_BF16) return launch_kv4_warp<__nv_bfloat16>(a, wplan, head_dim, batch, st);
+    return launch_kv4_warp<float>(a, wplan, head_dim, batch, st);
 }
 
 // ------------------------------------------------------------------------------------------
@@ -293,6 +352,10 @@ static cudaError_t stream_attributes() {
 }
 static cudaError_t set_kernel_attributes() {
     cudaError_t e;
+    if ((e = cudaFuncSetAttribute(kv4::kv4_attn_tc_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kv4::TC_SMEM)) != cudaSuccess) return e;
+    cudaFuncAttributes at;                       // its warpgroups share out the registers that it is launched with
+    if ((e = cudaFuncGetAttributes(&at, kv4::kv4_attn_tc_kernel)) != cudaSuccess) return e;
+    if (at.numRegs < kv4::TC_LAUNCH_REGS) return cudaErrorInvalidConfiguration;
     if ((e = stream_attributes<32, fp4::NV>()) != cudaSuccess || (e = stream_attributes<64, fp4::NV>()) != cudaSuccess) return e;
     if ((e = stream_attributes<128, fp4::NV>()) != cudaSuccess || (e = stream_attributes<32, fp4::MX>()) != cudaSuccess) return e;
     if ((e = stream_attributes<64, fp4::MX>()) != cudaSuccess || (e = stream_attributes<128, fp4::MX>()) != cudaSuccess) return e;

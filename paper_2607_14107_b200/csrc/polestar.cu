@@ -876,7 +876,9 @@ extern "C" int polestar_sm_count(void) {
     return g_last_sm_count;
 }
 
+namespace ps { void reload_operator_switches(); }        // operators.cu
 extern "C" int polestar_reload_env(void) {
+    reload_operator_switches();
     std::lock_guard<std::mutex> lk(g_mu);
     g_sw = read_switches();
     g_sw_loaded = true;

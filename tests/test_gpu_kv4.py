@@ -107,6 +107,20 @@ def test_attention(dtype, b, R, cap, nh, nkv, dh, lens):
     check(dtype, b, R, cap, nh, nkv, dh, lens)
 
 
+@pytest.mark.parametrize("kernel", [1, 2])
+@pytest.mark.parametrize("b,R,cap,nh,nkv,lens", [
+    (1, 1, 1, 1, 1, None), (2, 1, 700, 2, 1, [700, 130]), (3, 29, 1021, 4, 4, [1021, 0, 517]),       # one row tile: the streams split the keys
+    (2, 128, 129, 2, 2, [129, 128]), (1, 129, 127, 1, 1, None),                                        # a full row tile, a second one of a single row
+    (2, 70, 600, 7, 1, [600, 257]), (1, 520, 384, 1, 1, None), (2, 260, 1300, 2, 2, [1300, 3]),        # odd and even numbers of row tiles
+    (1, 3, 9000, 7, 1, [8999]), (2, 40, 5000, 4, 1, [5000, 700]),                                      # keys split over CTAs, some without any
+])
+def test_both_kernels(monkeypatch, kernel, b, R, cap, nh, nkv, lens):
+    monkeypatch.setenv("POLESTAR_KV4_KERNEL", str(kernel))
+    Bd.polestar_reload_env()
+    check("bf16", b, R, cap, nh, nkv, 128, lens, seed=kernel)
+    check("bf16", b, R, cap, nh, nkv, 128, lens, q_size=6.0, peaked=5.0, seed=kernel + 10)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("q_size,peaked", [(8.0, 6.0), (1e-4, 0.0), (3e4, 0.0), (1e-30, 0.0)])
 def test_attention_peaked_and_flat_rows(dtype, q_size, peaked):
