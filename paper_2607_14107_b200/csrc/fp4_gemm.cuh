@@ -225,5 +225,191 @@ gemm_stream_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
     if (warp == 1) tmem_dealloc(tmem, COLS);
 }
 
+// ---- many rows: bound by the tensor cores and by what L2 hands to them ----------------------------------------------------
+// A CTA pair (cluster of two, tcgen05 cta_group::2) works on a tile of 256 x 256 outputs: each CTA holds 128 rows of A and half of the tile's rows of B
+// in shared memory and its 128 rows x 256 columns of sums in its tensor memory; the even CTA issues the products for both.  Scales come as boxes of
+// whole blocks; every CTA needs those of its own rows of A and of all 256 rows of B.  Persistent: pairs take the tiles in an order in which those in
+// flight share their operands.  There is one accumulator (two of 256 columns would leave no tensor memory for scales): eight warps drain it into
+// registers, 128 columns each, and hand it back before they store.
+constexpr int PR_THREADS = 384;                  // warp 0: TMA, warp 1: MMA + tensor memory, warps 4..11: epilogue
+constexpr int PR_TILE = 256;
+constexpr int PR_STAGES = 5;
+__host__ __device__ constexpr uint32_t pr_stage_bytes(int fmt) { return 2 * 128 * 128 + 3 * scale_blocks(fmt) * BLOCK_BYTES; }
+__host__ __device__ constexpr size_t pr_smem_bytes(int fmt) { return 1024 + (size_t)PR_STAGES * ((pr_stage_bytes(fmt) + 1023) / 1024 * 1024); }
+static_assert(pr_smem_bytes(NV) <= 227 * 1024, "shared memory");
+
+__device__ __forceinline__ void copy_scales_pair(uint32_t tmem, uint64_t desc) {
+    asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" ::"r"(tmem), "l"(desc) : "memory");
+}
+template <int FMT>
+__device__ __forceinline__ void umma_fp4_pair(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t sa, uint32_t sb, uint32_t accumulate) {
+    if (FMT == NV)
+        asm volatile("{\n .reg .pred p;\n setp.ne.b32 p, %6, 0;\n"
+                     " tcgen05.mma.cta_group::2.kind::mxf4nvf4.block_scale.scale_vec::4X [%0], %1, %2, %3, [%4], [%5], p;\n}\n"
+                     ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(sa), "r"(sb), "r"(accumulate) : "memory");
+    else
+        asm volatile("{\n .reg .pred p;\n setp.ne.b32 p, %6, 0;\n"
+                     " tcgen05.mma.cta_group::2.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n}\n"
+                     ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(sa), "r"(sb), "r"(accumulate) : "memory");
+}
+// Tile number -> (row tile, column tile): chunks of 8 row tiles, inside which the row tile runs fastest, so that the pairs at work at one time cover a
+// compact block of the output.
+__device__ __forceinline__ void pair_tile(int id, int tiles_m, int tiles_n, int& tm, int& tn) {
+    const int per = 8 * tiles_n, chunk = id / per, local = id - chunk * per, rows = min(8, tiles_m - chunk * 8);
+    tn = local / rows;
+    tm = chunk * 8 + (local - tn * rows);
+}
+
+template <int FMT, typename OUT>
+__global__ void __launch_bounds__(PR_THREADS, 1)
+gemm_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ CUtensorMap map_as,
+                 const __grid_constant__ CUtensorMap map_bs, const __grid_constant__ GemmArgs g) {
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ uint64_t bars[2 * PR_STAGES + 2];
+    __shared__ uint32_t tmem_base_sh;
+    __shared__ int abort_sh;
+    constexpr int SB = scale_blocks(FMT);
+    constexpr uint32_t STAGE = (pr_stage_bytes(FMT) + 1023) / 1024 * 1024, B_OFF = 128 * 128, AS_OFF = 2 * B_OFF, BS_OFF = AS_OFF + SB * BLOCK_BYTES;
+    constexpr uint32_t SF_COL = 256;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int rank = (int)cluster_rank();
+    const int pair = (int)blockIdx.x >> 1, pairs = (int)gridDim.x >> 1;
+    const int tiles_m = (g.M + PR_TILE - 1) / PR_TILE, tiles_n = (g.N + PR_TILE - 1) / PR_TILE, tiles = tiles_m * tiles_n;
+    const int kbs = (g.K + KB - 1) / KB, sb_row = (g.K / group(FMT) + 3) / 4;
+
+    uint8_t* smem = (uint8_t*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
+    const uint32_t smem_base = smem_u32(smem), bar0 = smem_u32(&bars[0]);
+    auto full = [&](int s) { return bar0 + 8u * (uint32_t)s; };
+    auto empty = [&](int s) { return bar0 + 8u * (uint32_t)(PR_STAGES + s); };
+    const uint32_t acc_full = bar0 + 16u * PR_STAGES, acc_empty = acc_full + 8u;
+    volatile int* abort_flag = &abort_sh;
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < PR_STAGES; ++s) { mbar_init(full(s), 1); mbar_init(empty(s), 1); }
+        mbar_init(acc_full, 1);
+        mbar_init(acc_empty, 16);                // the epilogue warps of both CTAs
+        abort_sh = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    }
+    if (warp == 1) {
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_base_sh)), "r"(512u) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    }
+    tc_fence_before();
+    cluster_sync_all();                          // the peer's barriers exist before anything arrives on them
+    tc_fence_after();
+    pdl_trigger();
+    const uint32_t tmem = tmem_base_sh;
+
+    int issued = 0;
+    if (warp == 0) {
+        if (elect_one()) {
+            pdl_wait();
+            bool ok = true;
+            Ring r(0, PR_STAGES);
+            for (int id = pair; id < tiles && ok; id += pairs) {
+                int tm, tn;
+                pair_tile(id, tiles_m, tiles_n, tm, tn);
+                for (int kb = 0; kb < kbs && ok; ++kb, r.next(PR_STAGES)) {
+                    if (issued >= PR_STAGES) ok = mbar_wait(empty(r.slot), r.phase ^ 1u, abort_flag);
+                    if (!ok) break;
+                    const uint32_t slot = smem_base + (uint32_t)r.slot * STAGE, bar = mapa_u32(full(r.slot), 0);
+                    if (rank == 0) mbar_expect_tx(full(r.slot), 2 * pr_stage_bytes(FMT));      // of both CTAs
+                    tma_load_2d_pair(slot, &map_a, bar, kb * 128, (tm * 2 + rank) * 128);
+                    tma_load_2d_pair(slot + B_OFF, &map_b, bar, kb * 128, (tn * 2 + rank) * 128);
+                    tma_load_2d_pair(slot + AS_OFF, &map_as, bar, 0, (tm * 2 + rank) * sb_row + kb * SB);
+                    tma_load_2d_pair(slot + BS_OFF, &map_bs, bar, 0, (tn * 2) * sb_row + kb * SB);
+                    tma_load_2d_pair(slot + BS_OFF + SB * BLOCK_BYTES, &map_bs, bar, 0, (tn * 2 + 1) * sb_row + kb * SB);
+                    ++issued;
+                }
+            }
+        }
+    } else if (warp == 1) {
+        if (rank == 0 && elect_one()) {
+            bool ok = true;
+            Ring r(0, PR_STAGES);
+            int n = 0;                           // tiles of this pair
+            uint32_t set = 0;
+            for (int id = pair; id < tiles && ok; id += pairs, ++n) {
+                if (n > 0) ok = mbar_wait(acc_empty, (uint32_t)(n - 1) & 1u, abort_flag);
+                tc_fence_after();
+                for (int kb = 0; kb < kbs && ok; ++kb, r.next(PR_STAGES), set ^= 1u) {
+                    ok = mbar_wait(full(r.slot), r.phase, abort_flag);
+                    if (!ok) break;
+                    tc_fence_after();
+                    const uint32_t slot = smem_base + (uint32_t)r.slot * STAGE;
+                    const int steps = min(4, (g.K - kb * KB) / 64), blocks = min(SB, sb_row - kb * SB);
+                    const uint32_t sf_a = tmem + SF_COL + set * 64u, sf_b = sf_a + 16u;
+                    for (int c = 0; c < blocks; ++c) {
+                        copy_scales_pair(sf_a + 4u * (uint32_t)c, smem_desc_scales(slot + AS_OFF + (uint32_t)c * BLOCK_BYTES));
+                        copy_scales_pair(sf_b + 8u * (uint32_t)c, smem_desc_scales(slot + BS_OFF + (uint32_t)c * BLOCK_BYTES));
+                        copy_scales_pair(sf_b + 8u * (uint32_t)c + 4u, smem_desc_scales(slot + BS_OFF + (uint32_t)(SB + c) * BLOCK_BYTES));
+                    }
+                    const uint64_t da = smem_desc_sw128(slot), db = smem_desc_sw128(slot + B_OFF);
+                    for (int s = 0; s < steps; ++s) {
+                        const uint32_t c = (uint32_t)(FMT == NV ? s : s >> 1), byte = FMT == NV ? 0u : (uint32_t)(s & 1) * 2u;
+                        umma_fp4_pair<FMT>(tmem, da + (uint64_t)(2 * s), db + (uint64_t)(2 * s), instr_desc_fp4<FMT>(PR_TILE, PR_TILE, byte), sf_a + 4u * c,
+                                           sf_b + 8u * c, kb > 0 || s > 0 ? 1u : 0u);
+                    }
+                    umma_commit_pair(empty(r.slot));
+                }
+                umma_commit_pair(acc_full);      // (also on failure: the epilogue then sees the abort flag, or its own wait runs out)
+            }
+        }
+    } else if (warp >= 4) {
+        pdl_wait();
+        const float scale = (g.ta ? __ldg(g.ta) : 1.f) * (g.tb ? __ldg(g.tb) : 1.f);
+        const int quarter = warp & 3, half = (warp - 4) >> 2;
+        const uint32_t taddr = tmem + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(half * 128);
+        // rows of whole 16-byte pieces: vector stores
+        const bool vec = (((uintptr_t)g.out | (uintptr_t)(g.ld * (long long)sizeof(OUT))) & 15) == 0;
+        bool ok = true;
+        int n = 0;
+        for (int id = pair; id < tiles; id += pairs, ++n) {
+            int tm, tn;
+            pair_tile(id, tiles_m, tiles_n, tm, tn);
+            if (ok) ok = mbar_wait(acc_full, (uint32_t)n & 1u, abort_flag) && !*abort_flag;
+            ok = __all_sync(0xffffffffu, ok) != 0;
+            tc_fence_after();
+            uint32_t v[8][16];
+#pragma unroll
+            for (int c = 0; c < 8; ++c) tmem_ld16_issue(taddr + (uint32_t)(16 * c), v[c]);
+#pragma unroll
+            for (int c = 0; c < 8; ++c) tmem_ld_wait16(v[c]);
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive_cluster(mapa_u32(acc_empty, 0));
+            const long long m = (long long)(tm * 2 + rank) * 128 + quarter * 32 + lane;
+            const int n0 = tn * PR_TILE + half * 128;
+            if (m < g.M) {
+            OUT* dst = (OUT*)g.out + m * g.ld + n0;
+            const float nan = __uint_as_float(0x7fc00000u);      // a bounded wait gave up: NaN, not a partial sum
+#pragma unroll
+            for (int c = 0; c < 8; ++c) {
+                float f[16];
+#pragma unroll
+                for (int i = 0; i < 16; ++i) f[i] = ok ? __uint_as_float(v[c][i]) * scale : nan;
+                if (vec && n0 + 16 * c + 16 <= g.N) {
+                    store16<OUT>(dst + 16 * c, f);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) if (n0 + 16 * c + i < g.N) dst[16 * c + i] = from_f<OUT>(f[i]);
+                }
+            }
+            }
+            __syncwarp();
+        }
+    }
+    tc_fence_before();
+    __syncwarp();
+    if (abort_sh && issued > 0) {                // (the even CTA's barriers count the loads of both)
+        if (rank == 0) drain_ring(issued, PR_STAGES, bar0);
+        else for (const long long t0 = clock64(); clock64() - t0 < 4000000;) {}
+    }
+    cluster_sync_all();
+    if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
+}
+
 }  // namespace fp4
 }  // namespace ps

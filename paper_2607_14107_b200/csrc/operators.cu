@@ -32,11 +32,12 @@ static int switch_kv4() {
 
 // Facts of the CURRENT device; the first call on a device queries them and raises the shared-memory limits of the kernels that need
 // more than the default there (function attributes are per device).
-struct DevInfo { bool ready = false; int sm_count = 0; };
+struct DevInfo { bool ready = false; int sm_count = 0; int gemm_pairs = 0; };      // CTA pairs of the product that are resident at once
 static const int MAX_DEVICES = 64;
 static std::mutex g_mu;
 static DevInfo g_dev[MAX_DEVICES];
 static cudaError_t set_kernel_attributes();
+static int resident_gemm_pairs(int sms);
 static int device_info(DevInfo* out) {
     int dev = 0;
     CK(cudaGetDevice(&dev));
@@ -46,6 +47,7 @@ static int device_info(DevInfo* out) {
     if (!di.ready) {
         CK(cudaDeviceGetAttribute(&di.sm_count, cudaDevAttrMultiProcessorCount, dev));
         CK(set_kernel_attributes());
+        di.gemm_pairs = resident_gemm_pairs(di.sm_count);
         di.ready = true;
     }
     *out = di;
@@ -129,6 +131,31 @@ static bool make_code_map(CUtensorMap* out, const void* base, uint64_t rows, uin
               CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// blocks of 512 bytes of tiled scales: boxes of n blocks
+static bool make_scale_map(CUtensorMap* out, const void* base, uint64_t blocks, uint32_t n) {
+    EncodeTiledFn fn = get_encode_fn();
+    if (!fn) return false;
+    cuuint64_t dims[2] = {128, blocks};
+    cuuint64_t strides[1] = {fp4::BLOCK_BYTES};
+    cuuint32_t box[2] = {128, n};
+    cuuint32_t estr[2] = {1, 1};
+    return fn(out, CU_TENSOR_MAP_DATA_TYPE_UINT32, 2, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+              CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+template <int FMT, typename OUT>
+static int launch_gemm_pair(const uint8_t* a, const uint8_t* b, const fp4::GemmArgs& g, int pairs, cudaStream_t st) {
+    const uint64_t sb_row = ((uint64_t)g.K / fp4::group(FMT) + 3) / 4, rows_a = ((uint64_t)g.M + 127) / 128, rows_b = ((uint64_t)g.N + 127) / 128;
+    CUtensorMap ma, mb, mas, mbs;
+    if (!make_code_map(&ma, a, g.M, g.K / 2, 128) || !make_code_map(&mb, b, g.N, g.K / 2, 128) ||
+        !make_scale_map(&mas, g.as, rows_a * sb_row, fp4::scale_blocks(FMT)) || !make_scale_map(&mbs, g.bs, rows_b * sb_row, fp4::scale_blocks(FMT)))
+        return POLESTAR_E_CUDA;
+    const long long tiles = (((long long)g.M + fp4::PR_TILE - 1) / fp4::PR_TILE) * (((long long)g.N + fp4::PR_TILE - 1) / fp4::PR_TILE);
+    if (tiles > INT32_MAX / 2) return POLESTAR_E_INVAL;
+    const unsigned n = (unsigned)std::min<long long>(tiles, pairs);
+    CK(launch_k_cluster(fp4::gemm_pair_kernel<FMT, OUT>, dim3(2 * n), dim3(fp4::PR_THREADS), fp4::pr_smem_bytes(FMT), st, 2u, ma, mb, mas, mbs, g));
+    return POLESTAR_OK;
+}
+
 template <int T, int FMT, typename OUT>
 static int launch_gemm_stream(const uint8_t* a, const uint8_t* b, fp4::GemmArgs g, int sms, cudaStream_t st) {
     CUtensorMap ma, mb;
@@ -146,7 +173,8 @@ static int launch_gemm_stream(const uint8_t* a, const uint8_t* b, fp4::GemmArgs 
     return POLESTAR_OK;
 }
 template <int FMT, typename OUT>
-static int launch_gemm_fp4(const uint8_t* a, const uint8_t* b, const fp4::GemmArgs& g, int sms, cudaStream_t st) {
+static int launch_gemm_fp4(const uint8_t* a, const uint8_t* b, const fp4::GemmArgs& g, int sms, int pairs, cudaStream_t st) {
+    if (pairs > 0 && g.M > 128) return launch_gemm_pair<FMT, OUT>(a, b, g, pairs, st);
     if (g.M <= 32) return launch_gemm_stream<32, FMT, OUT>(a, b, g, sms, st);
     if (g.M <= 64) return launch_gemm_stream<64, FMT, OUT>(a, b, g, sms, st);
     return launch_gemm_stream<128, FMT, OUT>(a, b, g, sms, st);
@@ -170,8 +198,8 @@ extern "C" int polestar_k_fp4_matmul(const uint8_t* a_codes, const uint8_t* a_sc
     cudaStream_t st = (cudaStream_t)stream;
     const bool nv = format == POLESTAR_FP4_NV;
     if (out_dtype == POLESTAR_BF16)
-        return nv ? launch_gemm_fp4<fp4::NV, __nv_bfloat16>(a_codes, b_codes, g, di.sm_count, st) : launch_gemm_fp4<fp4::MX, __nv_bfloat16>(a_codes, b_codes, g, di.sm_count, st);
-    return nv ? launch_gemm_fp4<fp4::NV, float>(a_codes, b_codes, g, di.sm_count, st) : launch_gemm_fp4<fp4::MX, float>(a_codes, b_codes, g, di.sm_count, st);
+        return nv ? launch_gemm_fp4<fp4::NV, __nv_bfloat16>(a_codes, b_codes, g, di.sm_count, di.gemm_pairs, st) : launch_gemm_fp4<fp4::MX, __nv_bfloat16>(a_codes, b_codes, g, di.sm_count, di.gemm_pairs, st);
+    return nv ? launch_gemm_fp4<fp4::NV, float>(a_codes, b_codes, g, di.sm_count, di.gemm_pairs, st) : launch_gemm_fp4<fp4::MX, float>(a_codes, b_codes, g, di.sm_count, di.gemm_pairs, st);
 }
 
 // A cache of keys and values in 4 bits: what append and attention accept of its geometry.
@@ -350,8 +378,27 @@ static cudaError_t stream_attributes() {
     if (e == cudaSuccess) e = cudaFuncSetAttribute(fp4::gemm_stream_kernel<T, FMT, __nv_bfloat16>, cudaFuncAttributeMaxDynamicSharedMemorySize, n);
     return e;
 }
+template <int FMT>
+static cudaError_t pair_attributes() {
+    const int n = (int)fp4::pr_smem_bytes(FMT);
+    cudaError_t e = cudaFuncSetAttribute(fp4::gemm_pair_kernel<FMT, float>, cudaFuncAttributeMaxDynamicSharedMemorySize, n);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(fp4::gemm_pair_kernel<FMT, __nv_bfloat16>, cudaFuncAttributeMaxDynamicSharedMemorySize, n);
+    return e;
+}
+static int resident_gemm_pairs(int sms) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(2 * sms); cfg.blockDim = dim3(fp4::PR_THREADS); cfg.dynamicSmemBytes = fp4::pr_smem_bytes(fp4::NV);
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeClusterDimension;
+    at[0].val.clusterDim.x = 2; at[0].val.clusterDim.y = 1; at[0].val.clusterDim.z = 1;
+    cfg.attrs = at; cfg.numAttrs = 1;
+    int n = 0;
+    if (cudaOccupancyMaxActiveClusters(&n, fp4::gemm_pair_kernel<fp4::NV, __nv_bfloat16>, &cfg) != cudaSuccess) { cudaGetLastError(); return 0; }
+    return n;
+}
 static cudaError_t set_kernel_attributes() {
     cudaError_t e;
+    if ((e = pair_attributes<fp4::NV>()) != cudaSuccess || (e = pair_attributes<fp4::MX>()) != cudaSuccess) return e;
     if ((e = cudaFuncSetAttribute(kv4::kv4_attn_tc_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kv4::TC_SMEM)) != cudaSuccess) return e;
     cudaFuncAttributes at;                       // its warpgroups share out the registers that it is launched with
     if ((e = cudaFuncGetAttributes(&at, kv4::kv4_attn_tc_kernel)) != cudaSuccess) return e;

@@ -46,6 +46,16 @@ def test_products(M, N, K, fmt):
 
 
 @pytest.mark.parametrize("fmt", [F.NV, F.MX])
+@pytest.mark.parametrize("M,N,K,dtype", [
+    (256, 256, 256, torch.float32), (257, 255, 64, torch.float32), (1000, 1100, 2048, torch.bfloat16), (513, 20000, 448, torch.bfloat16),
+    (2100, 2500, 704, torch.float32), (997, 4099, 1600, torch.float32), (130, 30000, 1152, torch.bfloat16),
+])
+def test_products_of_many_rows(M, N, K, dtype, fmt):
+    # several tiles per CTA pair, ragged last tiles, K that ends inside a ring slot
+    check(M, N, K, fmt, dtype, seed=7)
+
+
+@pytest.mark.parametrize("fmt", [F.NV, F.MX])
 @pytest.mark.parametrize("M,N,K,pad", [(5, 131, 128, 3), (70, 515, 1088, 1), (260, 250, 512, 6)])
 def test_products_in_bf16_with_strided_rows(M, N, K, pad, fmt):
     check(M, N, K, fmt, torch.bfloat16, ld=N + pad, seed=3)
@@ -56,7 +66,7 @@ def test_products_in_bf16_with_strided_rows(M, N, K, pad, fmt):
 def test_codes_and_scales_meet(fmt):
     # one non-zero group per row, every group a scale and a code of its own: a product is right only if bytes, nibbles and scale ids are
     K, G = 512, F.group(fmt)
-    rows = 160
+    rows = 420
     c = np.zeros((rows, K), np.uint8)
     b = np.full((rows, K // G), 0 if fmt == F.NV else 1, np.uint8)
     for r in range(rows):
@@ -69,7 +79,7 @@ def test_codes_and_scales_meet(fmt):
     one_c = np.tile(np.array([2], np.uint8), (K, K)) * np.eye(K, dtype=np.uint8)        # code 2 is 1.0: the identity
     one_b = np.full((K, K // G), 56 if fmt == F.NV else 127, np.uint8)                   # scale 1.0
     eye_c, eye_s = torch.from_numpy(F.pack(one_c)).cuda(), torch.from_numpy(F.tile_scales(one_b)).cuda()
-    for M in (rows, 31, 64):
+    for M in (rows, 31, 64, 160):
         out = torch.zeros((M, K), device="cuda")
         a_scales = torch.from_numpy(F.tile_scales(b[:M])).cuda()
         Bd.polestar_k_fp4_matmul(codes[:M].contiguous(), a_scales, eye_c, eye_s, out, fmt)
