@@ -60,6 +60,7 @@ struct GemmArgs {
     void* out; long long ld;
     int M, N, K;
     int split;                                   // CTAs of a cluster that share the K of a tile
+    int box_out;                                 // output rows, their stride and base are whole 16 bytes: they leave as tensor stores
 };
 
 // ---- few rows of A: bound by the stream of B ---------------------------------------------------------------------------
@@ -230,14 +231,29 @@ gemm_stream_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
 // in shared memory and its 128 rows x 256 columns of sums in its tensor memory; the even CTA issues the products for both.  Scales come as boxes of
 // whole blocks; every CTA needs those of its own rows of A and of all 256 rows of B.  Persistent: pairs take the tiles in an order in which those in
 // flight share their operands.  There is one accumulator (two of 256 columns would leave no tensor memory for scales): eight warps drain it into
-// registers, 128 columns each, and hand it back before they store.
+// registers, 128 columns each, and hand it back before they store.  A lane has a row, so its stores would touch 32 lines per instruction (8192 cycles of
+// the load/store unit for a tile of fp32, more than its products take); rows of 128 bytes go through two swizzled boxes per warp and leave as tensor
+// stores.  Those write whole 16 bytes, also behind the last column: where a row's end or its stride is no multiple of that, the warp stores the boxes'
+// rows element by element.
 constexpr int PR_THREADS = 384;                  // warp 0: TMA, warp 1: MMA + tensor memory, warps 4..11: epilogue
 constexpr int PR_TILE = 256;
-constexpr int PR_STAGES = 5;
+constexpr int PR_STAGES = 4;
+constexpr uint32_t PR_BOX = 32 * 128;            // a box of outputs: 32 rows of 128 bytes, two of them per epilogue warp
 __host__ __device__ constexpr uint32_t pr_stage_bytes(int fmt) { return 2 * 128 * 128 + 3 * scale_blocks(fmt) * BLOCK_BYTES; }
-__host__ __device__ constexpr size_t pr_smem_bytes(int fmt) { return 1024 + (size_t)PR_STAGES * ((pr_stage_bytes(fmt) + 1023) / 1024 * 1024); }
+__host__ __device__ constexpr size_t pr_smem_bytes(int fmt) { return 1024 + (size_t)PR_STAGES * ((pr_stage_bytes(fmt) + 1023) / 1024 * 1024) + 8 * 2 * PR_BOX; }
 static_assert(pr_smem_bytes(NV) <= 227 * 1024, "shared memory");
 
+__device__ __forceinline__ void pack16(uint32_t (&w)[4], const float (&f)[4]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = __float_as_uint(f[i]);
+}
+__device__ __forceinline__ void pack16(uint32_t (&w)[4], const float (&f)[8]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const __nv_bfloat162 b = __floats2bfloat162_rn(f[2 * i], f[2 * i + 1]);
+        w[i] = *reinterpret_cast<const uint32_t*>(&b);
+    }
+}
 __device__ __forceinline__ void copy_scales_pair(uint32_t tmem, uint64_t desc) {
     asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" ::"r"(tmem), "l"(desc) : "memory");
 }
@@ -263,7 +279,7 @@ __device__ __forceinline__ void pair_tile(int id, int tiles_m, int tiles_n, int&
 template <int FMT, typename OUT>
 __global__ void __launch_bounds__(PR_THREADS, 1)
 gemm_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ CUtensorMap map_as,
-                 const __grid_constant__ CUtensorMap map_bs, const __grid_constant__ GemmArgs g) {
+                 const __grid_constant__ CUtensorMap map_bs, const __grid_constant__ CUtensorMap map_out, const __grid_constant__ GemmArgs g) {
     extern __shared__ uint8_t smem_raw[];
     __shared__ uint64_t bars[2 * PR_STAGES + 2];
     __shared__ uint32_t tmem_base_sh;
@@ -362,8 +378,8 @@ gemm_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
         const float scale = (g.ta ? __ldg(g.ta) : 1.f) * (g.tb ? __ldg(g.tb) : 1.f);
         const int quarter = warp & 3, half = (warp - 4) >> 2;
         const uint32_t taddr = tmem + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(half * 128);
-        // rows of whole 16-byte pieces: vector stores
-        const bool vec = (((uintptr_t)g.out | (uintptr_t)(g.ld * (long long)sizeof(OUT))) & 15) == 0;
+        constexpr int PER = 128 / sizeof(OUT), BOXES = 128 / PER;        // columns of a box, boxes of this warp's 128 columns
+        const uint32_t box0 = smem_base + PR_STAGES * STAGE + (uint32_t)(warp - 4) * (2 * PR_BOX);
         bool ok = true;
         int n = 0;
         for (int id = pair; id < tiles; id += pairs, ++n) {
@@ -380,26 +396,48 @@ gemm_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
             tc_fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive_cluster(mapa_u32(acc_empty, 0));
-            const long long m = (long long)(tm * 2 + rank) * 128 + quarter * 32 + lane;
-            const int n0 = tn * PR_TILE + half * 128;
-            if (m < g.M) {
-            OUT* dst = (OUT*)g.out + m * g.ld + n0;
+            const int m0 = (tm * 2 + rank) * 128 + quarter * 32, n0 = tn * PR_TILE + half * 128;
             const float nan = __uint_as_float(0x7fc00000u);      // a bounded wait gave up: NaN, not a partial sum
+            {
 #pragma unroll
-            for (int c = 0; c < 8; ++c) {
-                float f[16];
+                for (int x = 0; x < BOXES; ++x) {
+                    if (m0 >= g.M || n0 + x * PER >= g.N) break;             // (the same for all lanes)
+                    const uint32_t box = box0 + (uint32_t)(x & 1) * PR_BOX;
+                    if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");      // the store before the last has read its box
+                    __syncwarp();
 #pragma unroll
-                for (int i = 0; i < 16; ++i) f[i] = ok ? __uint_as_float(v[c][i]) * scale : nan;
-                if (vec && n0 + 16 * c + 16 <= g.N) {
-                    store16<OUT>(dst + 16 * c, f);
-                } else {
+                    for (int c = 0; c < 8; ++c) {                            // sixteen bytes of the lane's row
+                        uint32_t w[4];
+                        constexpr int E = 16 / sizeof(OUT);
+                        float f[E];
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) if (n0 + 16 * c + i < g.N) dst[16 * c + i] = from_f<OUT>(f[i]);
+                        for (int i = 0; i < E; ++i) { const int col = x * PER + c * E + i; f[i] = ok ? __uint_as_float(v[col >> 4][col & 15]) * scale : nan; }
+                        pack16(w, f);
+                        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(box + (uint32_t)lane * 128u + (uint32_t)((c ^ (lane & 7)) << 4)), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]) : "memory");
+                    }
+                    if (g.box_out) {
+                        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                        __syncwarp();
+                        if (lane == 0) {
+                            asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%2, %3}], [%1];" ::"l"(&map_out), "r"(box), "r"(n0 + x * PER), "r"(m0) : "memory");
+                            asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+                        }
+                    } else {
+                        __syncwarp();
+                        const uint8_t* sm = smem + (box - smem_base);
+                        const int rows = min(32, g.M - m0), cols = min(PER, g.N - n0 - x * PER);
+                        OUT* dst = (OUT*)g.out + (long long)m0 * g.ld + n0 + x * PER;
+                        for (int r = 0; r < rows; ++r, dst += g.ld)
+                            for (int c = lane; c < cols; c += 32) {
+                                const int byte = c * (int)sizeof(OUT);
+                                dst[c] = *reinterpret_cast<const OUT*>(sm + r * 128 + (((byte >> 4) ^ (r & 7)) << 4) + (byte & 15));
+                            }
+                    }
                 }
-            }
             }
             __syncwarp();
         }
+        if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
     }
     tc_fence_before();
     __syncwarp();

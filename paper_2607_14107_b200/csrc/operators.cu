@@ -142,17 +142,32 @@ static bool make_scale_map(CUtensorMap* out, const void* base, uint64_t blocks, 
     return fn(out, CU_TENSOR_MAP_DATA_TYPE_UINT32, 2, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
               CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
+// output rows of whole 16 bytes: boxes of 32 rows x 128 bytes, 128-byte swizzle
+static bool make_out_map(CUtensorMap* out, void* base, uint64_t rows, uint64_t cols, uint64_t ld, int es) {
+    EncodeTiledFn fn = get_encode_fn();
+    if (!fn) return false;
+    cuuint64_t dims[2] = {cols, rows};
+    cuuint64_t strides[1] = {ld * es};
+    cuuint32_t box[2] = {(cuuint32_t)(128 / es), 32};
+    cuuint32_t estr[2] = {1, 1};
+    return fn(out, es == 2 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 2, base, dims, strides, box, estr,
+              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
 template <int FMT, typename OUT>
-static int launch_gemm_pair(const uint8_t* a, const uint8_t* b, const fp4::GemmArgs& g, int pairs, cudaStream_t st) {
+static int launch_gemm_pair(const uint8_t* a, const uint8_t* b, fp4::GemmArgs g, int pairs, cudaStream_t st) {
     const uint64_t sb_row = ((uint64_t)g.K / fp4::group(FMT) + 3) / 4, rows_a = ((uint64_t)g.M + 127) / 128, rows_b = ((uint64_t)g.N + 127) / 128;
     CUtensorMap ma, mb, mas, mbs;
     if (!make_code_map(&ma, a, g.M, g.K / 2, 128) || !make_code_map(&mb, b, g.N, g.K / 2, 128) ||
         !make_scale_map(&mas, g.as, rows_a * sb_row, fp4::scale_blocks(FMT)) || !make_scale_map(&mbs, g.bs, rows_b * sb_row, fp4::scale_blocks(FMT)))
         return POLESTAR_E_CUDA;
+    // (strides of a tensor map stay below 2^40)
+    CUtensorMap mo = ma;
+    g.box_out = (((uintptr_t)g.out | (uintptr_t)(g.ld * (long long)sizeof(OUT)) | (uintptr_t)((size_t)g.N * sizeof(OUT))) & 15) == 0 && g.ld < (1LL << 36);
+    if (g.box_out && !make_out_map(&mo, g.out, g.M, g.N, g.ld, (int)sizeof(OUT))) return POLESTAR_E_CUDA;
     const long long tiles = (((long long)g.M + fp4::PR_TILE - 1) / fp4::PR_TILE) * (((long long)g.N + fp4::PR_TILE - 1) / fp4::PR_TILE);
     if (tiles > INT32_MAX / 2) return POLESTAR_E_INVAL;
     const unsigned n = (unsigned)std::min<long long>(tiles, pairs);
-    CK(launch_k_cluster(fp4::gemm_pair_kernel<FMT, OUT>, dim3(2 * n), dim3(fp4::PR_THREADS), fp4::pr_smem_bytes(FMT), st, 2u, ma, mb, mas, mbs, g));
+    CK(launch_k_cluster(fp4::gemm_pair_kernel<FMT, OUT>, dim3(2 * n), dim3(fp4::PR_THREADS), fp4::pr_smem_bytes(FMT), st, 2u, ma, mb, mas, mbs, mo, g));
     return POLESTAR_OK;
 }
 
@@ -194,7 +209,7 @@ extern "C" int polestar_k_fp4_matmul(const uint8_t* a_codes, const uint8_t* a_sc
     if (rc) return rc;
     fp4::GemmArgs g;
     g.as = a_scales; g.bs = b_scales; g.ta = a_tensor_scale; g.tb = b_tensor_scale; g.out = out; g.ld = ld_out;
-    g.M = M; g.N = N; g.K = K; g.split = 1;
+    g.M = M; g.N = N; g.K = K; g.split = 1; g.box_out = 0;
     cudaStream_t st = (cudaStream_t)stream;
     const bool nv = format == POLESTAR_FP4_NV;
     if (out_dtype == POLESTAR_BF16)
