@@ -6,33 +6,48 @@
 //
 // A thread-block cluster of up to eight CTAs per row, as in the confidence kernel; every thread carries (m, S, Q) in 32 bits and
 // rescales once per batch of loads.  Alternatives: the k-th largest of the maxima of 64 groups of threads is a lower bound of the k-th largest
-// logit, so only threads whose own maximum reaches it look at their logits again; what reaches the bound goes through a buffer in shared
-// memory as (value, index) keys, whose order is total: larger values first, lower indices first among equals.  If the buffer overflows (many equal
+// logit, so only the pieces of threads whose own maximum reaches it are read again, dealt out over the whole CTA; what reaches the bound goes through a
+// buffer in shared memory as (value, index) keys, whose order is total: larger values first, lower indices first among equals.  If the buffer overflows (many equal
 // logits), its own k-th key is a higher bound, and the collection runs again; every round drops all but k of a full buffer, so it ends.
 #pragma once
-#include "common.cuh"
+#include "tcgen05.cuh"
 
 namespace ps {
 namespace lpr {
 
+using namespace tc;
+
 constexpr int MAX_CL = 8, MAX_THREADS = 512, MAX_K = 32, SEGMENTS = 64, CAP = 1024, U = 4;
 
+// Sixteen bytes of logits: unpacked as they are, unpacked with -inf as the lowest finite value (NaN stays), and their largest (NaN left out).
 template <typename T> struct In;
 template <> struct In<float> {
     static constexpr int N = 4;
+    static constexpr uint32_t PAD = 0xff800000u;       // a piece that is not there: -inf
     static __device__ __forceinline__ void unpack(const uint4& w, float* v) {
         v[0] = __uint_as_float(w.x); v[1] = __uint_as_float(w.y); v[2] = __uint_as_float(w.z); v[3] = __uint_as_float(w.w);
     }
-    static constexpr uint32_t PAD = 0xff800000u;       // a piece that is not there: -inf
+    static __device__ __forceinline__ void finite(const uint4& w, float* v) {
+        unpack(w, v);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) asm("max.NaN.f32 %0, %0, %1;" : "+f"(v[i]) : "f"(-3.4028234663852886e38f));
+    }
+    static __device__ __forceinline__ float top(const uint4& w) {
+        return fmaxf(fmaxf(__uint_as_float(w.x), __uint_as_float(w.y)), fmaxf(__uint_as_float(w.z), __uint_as_float(w.w)));
+    }
 };
 template <> struct In<__nv_bfloat16> {
     static constexpr int N = 8;
-    static __device__ __forceinline__ void unpack(const uint4& w, float* v) {
-        const uint32_t x[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) { v[2 * i] = __uint_as_float(x[i] << 16); v[2 * i + 1] = __uint_as_float(x[i] & 0xffff0000u); }
-    }
     static constexpr uint32_t PAD = 0xff80ff80u;
+    static __device__ __forceinline__ void spread(uint32_t x, float* v) { v[0] = __uint_as_float(x << 16); v[1] = __uint_as_float(x & 0xffff0000u); }
+    static __device__ __forceinline__ void unpack(const uint4& w, float* v) { spread(w.x, v); spread(w.y, v + 2); spread(w.z, v + 4); spread(w.w, v + 6); }
+    static __device__ __forceinline__ uint32_t low(uint32_t x) { uint32_t y; asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(y) : "r"(x), "r"(0xff7fff7fu)); return y; }
+    static __device__ __forceinline__ void finite(const uint4& w, float* v) { spread(low(w.x), v); spread(low(w.y), v + 2); spread(low(w.z), v + 4); spread(low(w.w), v + 6); }
+    static __device__ __forceinline__ uint32_t max2(uint32_t x, uint32_t y) { uint32_t z; asm("max.bf16x2 %0, %1, %2;" : "=r"(z) : "r"(x), "r"(y)); return z; }
+    static __device__ __forceinline__ float top(const uint4& w) {
+        const uint32_t m = max2(max2(w.x, w.y), max2(w.z, w.w));
+        return fmaxf(__uint_as_float(m << 16), __uint_as_float(m & 0xffff0000u));
+    }
 };
 
 struct Args {
@@ -42,12 +57,25 @@ struct Args {
     int V, mask_id, k, cl;
 };
 
+// the value's place in the order of its type, as an integer (0 below all values; NaN's is not used)
+__device__ __forceinline__ uint32_t order(float x) {
+    const uint32_t b = __float_as_uint(x + 0.f);         // (-0 counts as 0)
+    return (b & 0x80000000u) ? ~b : b | 0x80000000u;
+}
+// sums over the sixteen lanes of a half warp, every lane of the warp taking part
+__device__ __forceinline__ int sum16(int v) {
+#pragma unroll
+    for (int o = 8; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    return v;
+}
+__device__ __forceinline__ int above16(const unsigned long long* list, int n, unsigned long long key, int lane16) {
+    int c = 0;
+    for (int j = lane16; j < n; j += 16) c += list[j] > key;
+    return sum16(c);
+}
 // (value, index) as one integer: larger is earlier.  -0 counts as 0; NaN is never an alternative (key 0).
 __device__ __forceinline__ unsigned long long make_key(float x, int v) {
-    if (x != x) return 0ull;
-    const uint32_t b = __float_as_uint(x + 0.f);
-    const uint32_t o = (b & 0x80000000u) ? ~b : b | 0x80000000u;
-    return ((unsigned long long)o << 32) | (uint32_t)~v;
+    return x != x ? 0ull : ((unsigned long long)order(x) << 32) | (uint32_t)~v;
 }
 __device__ __forceinline__ float key_value(unsigned long long k) {
     const uint32_t o = (uint32_t)(k >> 32);
@@ -55,7 +83,7 @@ __device__ __forceinline__ float key_value(unsigned long long k) {
 }
 __device__ __forceinline__ int key_index(unsigned long long k) { return (int)~(uint32_t)k; }
 
-__device__ __forceinline__ float ex2(float x) { float y; asm("ex2.approx.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
+__device__ __forceinline__ float ex2(float x) { float y; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
 constexpr float L2E = 1.4426950408889634f;
 
 struct Run {
@@ -77,10 +105,11 @@ __global__ void __launch_bounds__(MAX_THREADS) token_logprobs_kernel(Args a) {
     constexpr int N = In<T>::N;
     __shared__ float4 parts[MAX_CL * (MAX_THREADS / 32)];
     __shared__ unsigned long long tops[MAX_CL * MAX_K];
-    __shared__ unsigned long long seg[SEGMENTS];
+    __shared__ uint32_t seg[SEGMENTS];
     __shared__ unsigned long long buf[CAP];
     __shared__ unsigned long long bound_sh;
-    __shared__ int n_sh;
+    __shared__ int n_sh, own_n;
+    __shared__ unsigned short own[MAX_THREADS];
     const int cl = a.cl, row = (int)blockIdx.x / cl, ch = (int)blockIdx.x - row * cl;
     // (the first CTA must run before anything is pushed into its shared memory: the barrier passes under the loads)
     if (cl > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
@@ -101,14 +130,9 @@ __global__ void __launch_bounds__(MAX_THREADS) token_logprobs_kernel(Args a) {
         uint4 w[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) w[u] = i + u * nt < c1 ? __ldg(l4 + i + u * nt) : make_uint4(In<T>::PAD, In<T>::PAD, In<T>::PAD, In<T>::PAD);
-        float bm = -INFINITY;
+        float bm = In<T>::top(w[0]);
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            float v[N];
-            In<T>::unpack(w[u], v);
-#pragma unroll
-            for (int e = 0; e < N; ++e) bm = fmaxf(bm, v[e]);
-        }
+        for (int u = 1; u < U; ++u) bm = fmaxf(bm, In<T>::top(w[u]));
         // the mask token is no alternative: only the batch that holds it looks
         float bb = bm;
         const int vm = a.mask_id - lead - i * N;
@@ -123,62 +147,75 @@ __global__ void __launch_bounds__(MAX_THREADS) token_logprobs_kernel(Args a) {
             }
         }
         best = fmaxf(best, bb);
-        const float nm = fmaxf(r.m, bm), ref = nm == -INFINITY ? 0.f : nm;
-        const float d = fmaxf(r.m - ref, -1e30f), f = ex2(d * L2E);
-        r.q = f * (r.q + r.s * d);
-        r.s *= f;
-        r.m = nm;
-        float s2[2] = {0.f, 0.f}, q2[2] = {0.f, 0.f};
+        if (bm > r.m) {                                  // (rare after the first batches)
+            const float d = fmaxf(r.m - bm, -1e30f), f = ex2(d * L2E);
+            r.q = f * (r.q + r.s * d);
+            r.s *= f;
+            r.m = bm;
+        }
+        if (__builtin_expect(r.m >= -1e38f, 1)) {
+            // -inf as the lowest finite value: p = 0 all the same, and p z = 0
+            const uint64_t nm2 = f2_pack(-r.m, -r.m), l2e = f2_pack(L2E, L2E);
+            uint64_t s2[2] = {0ull, 0ull}, q2[2] = {0ull, 0ull};
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            float v[N];
-            In<T>::unpack(w[u], v);
+            for (int u = 0; u < U; ++u) {
+                float v[N];
+                In<T>::finite(w[u], v);
 #pragma unroll
-            for (int e = 0; e < N; ++e) {
-                const float z = fmaxf(v[e] - ref, -1e30f);           // (-inf: e^z = 0, and 0 * z = 0)
-                const float p = ex2(z * L2E);
-                const float pn = v[e] == v[e] ? p : v[e];            // (the maximum of NaN and a number is the number)
-                s2[e & 1] += pn;
-                q2[e & 1] = fmaf(p, z, q2[e & 1]);
+                for (int e = 0; e < N; e += 2) {
+                    const uint64_t d = f2_add(f2_pack(v[e], v[e + 1]), nm2);
+                    float z0, z1;
+                    f2_unpack(f2_mul(d, l2e), z0, z1);
+                    const uint64_t p = f2_pack(ex2(z0), ex2(z1));
+                    s2[(e >> 1) & 1] = f2_add(s2[(e >> 1) & 1], p);
+                    q2[(e >> 1) & 1] = f2_fma(p, d, q2[(e >> 1) & 1]);
+                }
+            }
+            r.s += f2_sum(f2_add(s2[0], s2[1]));
+            r.q += f2_sum(f2_add(q2[0], q2[1]));
+        } else {                                         // (nothing above the lowest values so far: -inf is told from them)
+            const float ref = r.m == -INFINITY ? 0.f : r.m;
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                float v[N];
+                In<T>::unpack(w[u], v);
+#pragma unroll
+                for (int e = 0; e < N; ++e) {
+                    const float z = fmaxf(v[e] - ref, -1e30f), p = v[e] == v[e] ? (v[e] == -INFINITY ? 0.f : ex2(z * L2E)) : v[e];
+                    r.s += p;
+                    r.q += p * z;
+                }
             }
         }
-        r.s += s2[0] + s2[1];
-        r.q += q2[0] + q2[1];
     }
     if (extra >= 0) r.join(x_extra, x_extra == x_extra ? (x_extra > -INFINITY ? 1.f : 0.f) : x_extra, 0.f);
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1)
         r.join(__shfl_xor_sync(0xffffffffu, r.m, o), __shfl_xor_sync(0xffffffffu, r.s, o), __shfl_xor_sync(0xffffffffu, r.q, o));
 
-    // ---- the CTA's k largest alternatives, in order, into tops[ch * MAX_K ..] of the first CTA ----
-    unsigned long long mine = 0;                         // the key that thread t < k hands on
+    // ---- the CTA's k largest alternatives: candidates in buf[0 .. n) ----
+    int n = 0;
     if (a.k > 0) {
         // lower bound from the maxima of up to 64 groups of neighbouring threads (values only: equal ones are sorted out below)
-        unsigned long long key = make_key(best, 0) | 0xffffffffull;
-        if (c0 + t >= c1 && extra < 0) key = 0;          // a thread without logits
+        const uint32_t mine = c0 + t < c1 || extra >= 0 ? order(best) : 0u;            // (0: a thread without logits)
+        uint32_t top = mine;
         const int width = max(1, nt / SEGMENTS);         // 1, 2, 4 or 8 threads
-        for (int o = 1; o < width; o <<= 1) {
-            const unsigned long long other = __shfl_xor_sync(0xffffffffu, key, o);
-            key = other > key ? other : key;
-        }
-        if (t < SEGMENTS) seg[t] = 0;
-        if (t == 0) bound_sh = 0;
+        for (int o = 1; o < width; o <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
+        if (nt < SEGMENTS * width && t < SEGMENTS) seg[t] = 0;
+        if (t == 0) { bound_sh = 0; n_sh = 0; own_n = 0; }
         __syncthreads();
-        if (t % width == 0) seg[t / width] = key;
+        if (t % width == 0) seg[t / width] = top;
         __syncthreads();
-        if (t < SEGMENTS) {
-            const unsigned long long k0 = seg[t];
+        for (int i = t >> 4; i < SEGMENTS; i += nt >> 4) {
+            const uint32_t s0 = seg[i];
             int above = 0;
-            for (int i = 0; i < SEGMENTS; ++i) above += seg[i] > k0 || (seg[i] == k0 && i < t);
-            if (above == a.k - 1) bound_sh = k0 & 0xffffffff00000000ull;       // (values equal to it are candidates)
+#pragma unroll
+            for (int j = 0; j < SEGMENTS; j += 16) { const uint32_t s1 = seg[j + (t & 15)]; above += s1 > s0 || (s1 == s0 && j + (t & 15) < i); }
+            if (sum16(above) == a.k - 1 && (t & 15) == 0) bound_sh = (unsigned long long)s0 << 32;       // (values equal to it are candidates)
         }
         __syncthreads();
         unsigned long long bound = bound_sh;
-        int n;
         while (true) {
-            __syncthreads();
-            if (t == 0) n_sh = 0;
-            __syncthreads();
             auto offer = [&](float x, int v) {
                 const unsigned long long k1 = make_key(x, v);
                 if (v != a.mask_id && k1 >= bound && k1 != 0) {
@@ -186,50 +223,51 @@ __global__ void __launch_bounds__(MAX_THREADS) token_logprobs_kernel(Args a) {
                     if (at < CAP) buf[at] = k1;
                 }
             };
-            // a thread whose maximum reaches the bound: its pieces are read by the lanes of its warp side by side
-            const bool look = c0 + t < c1 && (make_key(best, 0) | 0xffffffffull) >= bound;
-            for (unsigned todo = __ballot_sync(0xffffffffu, look); todo; todo &= todo - 1) {
-                const int owner = wid * 32 + __ffs(todo) - 1;
-                for (int i = c0 + owner + lane * nt; i < c1; i += 32 * nt) {
-                    const uint4 w = __ldg(l4 + i);
-                    float v[N];
-                    In<T>::unpack(w, v);
+            // the pieces of the threads whose maximum reaches the bound, over all threads of the CTA
+            if (c0 + t < c1 && mine >= (uint32_t)(bound >> 32)) own[atomicAdd(&own_n, 1)] = (unsigned short)t;
+            __syncthreads();
+            const int each = (c1 - c0 + nt - 1) / nt, items = own_n * each;
+            for (int i = t; i < items; i += nt) {
+                const int o = i / each, at = c0 + own[o] + (i - o * each) * nt;
+                if (at >= c1) continue;
+                const uint4 w = __ldg(l4 + at);
+                if (order(In<T>::top(w)) < (uint32_t)(bound >> 32)) continue;
+                float v[N];
+                In<T>::unpack(w, v);
 #pragma unroll
-                    for (int e = 0; e < N; ++e) offer(v[e], lead + i * N + e);
-                }
+                for (int e = 0; e < N; ++e) offer(v[e], lead + at * N + e);
             }
             if (extra >= 0) offer(x_extra, extra);
             __syncthreads();
             n = n_sh;
             if (n <= CAP) break;
             // a full buffer: its k-th key bounds the k-th of the row from below
-            for (int i = t; i < CAP; i += nt) {
+            for (int i = t >> 4; i < CAP; i += nt >> 4) {
                 const unsigned long long k0 = buf[i];
-                int above = 0;
-                for (int j = 0; j < CAP; ++j) above += buf[j] > k0;
-                if (above == a.k - 1) bound_sh = k0;
+                if (above16(buf, CAP, k0, t & 15) == a.k - 1 && (t & 15) == 0) bound_sh = k0;
             }
             __syncthreads();
             bound = bound_sh;
+            if (t == 0) { n_sh = 0; own_n = 0; }
+            __syncthreads();
         }
-        for (int i = t; i < n; i += nt) {
-            const unsigned long long k0 = buf[i];
-            int above = 0;
-            for (int j = 0; j < n; ++j) above += buf[j] > k0;
-            if (above < a.k) seg[above] = k0;            // (keys are distinct: every place is taken once)
-        }
-        __syncthreads();
-        if (t < a.k) mine = t < n ? seg[t] : 0ull;
     }
 
+    // parts and alternatives, these in order, into the first CTA's shared memory
     if (cl > 1) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
     if (lane == 0) {
         const uint32_t dst = dsmem_addr((uint32_t)__cvta_generic_to_shared(parts + ch * nw + wid), 0);
         asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(dst), "f"(r.m), "f"(r.s), "f"(r.q), "f"(0.f) : "memory");
     }
-    if (t < a.k) {
-        const uint32_t dst = dsmem_addr((uint32_t)__cvta_generic_to_shared(tops + ch * a.k + t), 0);
-        asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(dst), "l"(mine) : "memory");
+    if (a.k > 0) {
+        const uint32_t list = dsmem_addr((uint32_t)__cvta_generic_to_shared(tops + ch * a.k), 0);
+        auto put = [&](int at, unsigned long long key) { asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(list + 8u * (uint32_t)at), "l"(key) : "memory"); };
+        for (int i = t >> 4; i < (n + 1) / 2 * 2; i += nt >> 4) {             // (both halves of a warp, or neither)
+            const unsigned long long k0 = i < n ? buf[i] : 0ull;
+            const int above = above16(buf, n, k0, t & 15);
+            if (i < n && above < a.k && (t & 15) == 0) put(above, k0);       // (keys are distinct: every place is taken once)
+        }
+        if (t >= n && t < a.k) put(t, 0ull);
     }
     if (cl > 1) cluster_sync_all(); else __syncthreads();
     if (ch != 0) return;
@@ -239,6 +277,7 @@ __global__ void __launch_bounds__(MAX_THREADS) token_logprobs_kernel(Args a) {
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1)
         f.join(__shfl_xor_sync(0xffffffffu, f.m, o), __shfl_xor_sync(0xffffffffu, f.s, o), __shfl_xor_sync(0xffffffffu, f.q, o));
+    if (f.m > 1e30f) f.q = 0.f;          // floats there are 1e22 apart: p is 1 or 0, and Q exactly 0 (p z may have been 0 * inf)
     const float ls = logf(f.s);
     // (a row without an entry above -inf, or with an infinite one: S = 0; one with NaN: S is NaN.  All its results are NaN.)
     if (t == 0) {
@@ -251,10 +290,14 @@ __global__ void __launch_bounds__(MAX_THREADS) token_logprobs_kernel(Args a) {
             a.logprob[row] = lp;
         }
     }
-    for (int i = t; i < cl * a.k; i += nt) {
-        const unsigned long long k0 = tops[i];
+    // places of the CTAs' alternatives among all of them (keys of 0 are places that none took: they come last, behind one another)
+    const int all = cl * a.k;
+    for (int i = t >> 4; i < (all + 1) / 2 * 2; i += nt >> 4) {
+        const unsigned long long k0 = i < all ? tops[i] : 0ull;
         int above = 0;
-        for (int j = 0; j < cl * a.k; ++j) above += tops[j] > k0 || (tops[j] == k0 && j < i);
+        for (int j = t & 15; j < all; j += 16) above += tops[j] > k0 || (tops[j] == k0 && j < i);
+        above = sum16(above);
+        if (i >= all || (t & 15) != 0) continue;
         if (above >= a.k) continue;
         const size_t at = (size_t)row * a.k + above;
         a.top_ids[at] = k0 ? key_index(k0) : -1;         // fewer alternatives than asked for
