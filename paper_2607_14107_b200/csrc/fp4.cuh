@@ -11,10 +11,14 @@
 // Bound by the copy at thousands of rows, by latency at a block of rows.  A lane holds 16 bytes of a row (4 or 8 channels), so every
 // load and store of a warp is contiguous whatever the type; the lanes of a group find its maximum by shuffles.
 #pragma once
-#include "common.cuh"
+#include <cuda_fp16.h>
+
+#include "tcgen05.cuh"
 
 namespace ps {
 namespace fp4 {
+
+using namespace tc;
 
 enum { NV = 0, MX = 1 };
 enum { ROWS = 0, TILED = 1 };
@@ -28,34 +32,45 @@ __device__ __forceinline__ size_t tiled_offset(long long r, int g, int g4) {
     return ((size_t)(r >> 7) * g4 + (g >> 2)) * 512 + (size_t)((r & 31) * 16 + ((r >> 5) & 3) * 4 + (g & 3));
 }
 
+// Correctly rounded quotients by a divisor b with r = RN(1 / b): q = x r is within an ulp, and one step q + (x - b q) r rounds correctly (Markstein,
+// 1990) while nothing overflows or underflows: |b| and |x| within 2^-100 .. 2^100 (x = 0 too).
+__device__ __forceinline__ float divide(float x, float b, float r) {
+    const float q = x * r;
+    return fmaf(fmaf(-b, q, x), r, q);
+}
+__device__ __forceinline__ bool in_range(float x) { return x >= FAST_LO && x <= FAST_HI; }
+
+// the tensor's factor and what follows from it alone
+struct Factor {
+    float t, b, r;                               // b: divisor of a group's maximum (6 t or t), r = RN(1 / b)
+    bool fast;
+};
+template <int FMT> __device__ __forceinline__ Factor make_factor(const float* p) {
+    Factor f;
+    f.t = p ? __ldg(p) : 1.f;
+    f.b = FMT == NV ? __fmul_rn(f.t, 6.f) : f.t;
+    f.r = __frcp_rn(f.b);
+    f.fast = in_range(f.b);
+    return f;
+}
 // scale of a group from the largest magnitude's bits (an integer maximum: NaN and infinity stay on top)
 template <int FMT>
-__device__ __forceinline__ float group_scale(uint32_t amax, float t, uint32_t* byte) {
-    if (amax >= 0x7f800000u) {
-        *byte = FMT == NV ? 0x7fu : 0xffu;
-        return __uint_as_float(0x7fc00000u);
-    }
+__device__ __forceinline__ float group_scale(uint32_t amax, const Factor& f, uint32_t* byte) {
+    const float a = __uint_as_float(amax);
+    float q = f.fast && in_range(a) ? divide(a, f.b, f.r) : __fdiv_rn(a, f.b);
     if (FMT == NV) {
-        const float s = e4m3_round_pos(__fdiv_rn(__uint_as_float(amax), __fmul_rn(t, 6.f)));
-        *byte = e4m3_bits(s);
-        return s;
+        if (amax >= 0x7f800000u) q = __uint_as_float(0x7fc00000u);
+        uint16_t e;
+        uint32_t h;
+        asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(e) : "f"(0.f), "f"(q));
+        asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"(e));
+        *byte = e;
+        return __half2float(__ushort_as_half((unsigned short)h));
     }
-    const int e = (int)(__float_as_uint(__fdiv_rn(__uint_as_float(amax), t)) >> 23);          // biased; 255: the quotient is beyond fp32
-    const uint32_t b = e == 255 ? 254u : (uint32_t)max(e - 2, 0);
+    const int e = (int)(__float_as_uint(q) >> 23);                     // biased; 255: the quotient is beyond fp32
+    const uint32_t b = amax >= 0x7f800000u ? 255u : e == 255 ? 254u : (uint32_t)max(e - 2, 0);
     *byte = b;
-    return b == 0 ? __uint_as_float(0x00400000u) : __uint_as_float(b << 23);
-}
-
-// Two codes (low nibble first) of x0, x1 in a group with unit u = s t > 0 and r = its correctly rounded reciprocal.  The quotients are
-// the IEEE ones: q = x r is within an ulp, and one step q + (x - u q) r rounds correctly (Markstein, 1990) while nothing overflows or
-// underflows; a unit far out, where that could happen, divides.  The conversion rounds to nearest, ties to the even code, and saturates.
-__device__ __forceinline__ uint32_t code_pair(float x0, float x1, float u, float r, bool fast) {
-    if (!fast) return e2m1_code(x0, u) | (e2m1_code(x1, u) << 4);
-    const float q0 = x0 * r, q1 = x1 * r;
-    const float y0 = fmaf(fmaf(-u, q0, x0), r, q0), y1 = fmaf(fmaf(-u, q1, x1), r, q1);
-    uint32_t c;
-    asm("{\n .reg .b8 b;\n cvt.rn.satfinite.e2m1x2.f32 b, %2, %1;\n mov.b32 %0, {b, 0, 0, 0};\n}\n" : "=r"(c) : "f"(y0), "f"(y1));
-    return c;
+    return amax >= 0x7f800000u ? __uint_as_float(0x7fc00000u) : b == 0 ? __uint_as_float(0x00400000u) : __uint_as_float(b << 23);
 }
 
 template <typename T> struct Vec;                                     // 16 bytes of a row
@@ -63,6 +78,9 @@ template <> struct Vec<float> {
     static constexpr int N = 4;
     static __device__ __forceinline__ void unpack(const uint4& w, float* v) {
         v[0] = __uint_as_float(w.x); v[1] = __uint_as_float(w.y); v[2] = __uint_as_float(w.z); v[3] = __uint_as_float(w.w);
+    }
+    static __device__ __forceinline__ uint32_t amax(const uint4& w) {        // bits of the largest magnitude as a float
+        return max(max(w.x & 0x7fffffffu, w.y & 0x7fffffffu), max(w.z & 0x7fffffffu, w.w & 0x7fffffffu));
     }
     static __device__ __forceinline__ uint4 pack(const float* v) {
         return make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
@@ -74,6 +92,11 @@ template <> struct Vec<__nv_bfloat16> {
         const uint32_t x[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
         for (int i = 0; i < 4; ++i) { v[2 * i] = __uint_as_float(x[i] << 16); v[2 * i + 1] = __uint_as_float(x[i] & 0xffff0000u); }
+    }
+    static __device__ __forceinline__ uint32_t max2(uint32_t x, uint32_t y) { uint32_t z; asm("max.u16x2 %0, %1, %2;" : "=r"(z) : "r"(x), "r"(y)); return z; }
+    static __device__ __forceinline__ uint32_t amax(const uint4& w) {
+        const uint32_t m = max2(max2(w.x & 0x7fff7fffu, w.y & 0x7fff7fffu), max2(w.z & 0x7fff7fffu, w.w & 0x7fff7fffu));
+        return max(m << 16, m & 0xffff0000u);
     }
     static __device__ __forceinline__ uint4 pack(const float* v) {
         uint32_t x[4];
@@ -87,31 +110,44 @@ template <> struct Vec<__nv_bfloat16> {
 };
 
 // One lane's 16 bytes of a group (all lanes of the warp take part; the lanes of a group are neighbours): the codes, four bits each, channel
-// 0 lowest, the group's scale byte, and the stored values in the row's type.
+// 0 lowest, the group's scale byte, and the stored values in the row's type.  The conversion to E2M1 rounds to nearest, ties to the even code, and
+// saturates; groups whose unit s t is so far out that the division's steps could overflow or underflow divide by the instruction.
 template <typename T, int FMT>
-__device__ __forceinline__ uint32_t encode(const uint4& w, float t, uint32_t* byte, uint4* stored) {
+__device__ __forceinline__ uint32_t encode(const uint4& w, const Factor& f, uint32_t* byte, uint4* stored) {
     constexpr int N = Vec<T>::N, LANES = group(FMT) / N;
-    float v[N];
-    Vec<T>::unpack(w, v);
-    uint32_t am = 0;
-#pragma unroll
-    for (int i = 0; i < N; ++i) am = max(am, __float_as_uint(v[i]) & 0x7fffffffu);
+    uint32_t am = Vec<T>::amax(w);
 #pragma unroll
     for (int o = 1; o < LANES; o <<= 1) am = max(am, __shfl_xor_sync(0xffffffffu, am, o));
-    const float s = group_scale<FMT>(am, t, byte);
-    const float u = __fmul_rn(s, t);
-    const bool fast = u >= FAST_LO && u <= FAST_HI;
+    const float s = group_scale<FMT>(am, f, byte);
+    const float u = __fmul_rn(s, f.t);
+    float v[N];
+    Vec<T>::unpack(w, v);
     uint32_t codes = 0;
-    if (s > 0.f) {
+    if (__builtin_expect(in_range(u), 1)) {
         const float r = __frcp_rn(u);
+        const uint64_t r2 = f2_pack(r, r), nu = f2_pack(-u, -u);
+        uint32_t c[4] = {0, 0, 0, 0};
 #pragma unroll
-        for (int i = 0; i < N; i += 2) codes |= code_pair(v[i], v[i + 1], u, r, fast) << (4 * i);
+        for (int i = 0; i < N / 2; ++i) {
+            const uint64_t x = f2_pack(v[2 * i], v[2 * i + 1]), q = f2_mul(x, r2);
+            float y0, y1;
+            f2_unpack(f2_fma(f2_fma(nu, q, x), r2, q), y0, y1);
+            asm("{\n .reg .b8 b;\n cvt.rn.satfinite.e2m1x2.f32 b, %2, %1;\n mov.b32 %0, {b, 0, 0, 0};\n}\n" : "=r"(c[i]) : "f"(y0), "f"(y1));
+        }
+        codes = c[0] | (c[1] << 8) | (c[2] << 16) | (c[3] << 24);
+    } else if (s > 0.f) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) codes |= e2m1_code(v[i], u) << (4 * i);
     }
     if (stored) {
+        uint32_t h[4];
+        asm("{\n .reg .b8 a, b, c, d;\n mov.b32 {a, b, c, d}, %4;\n cvt.rn.f16x2.e2m1x2 %0, a;\n cvt.rn.f16x2.e2m1x2 %1, b;\n"
+            " cvt.rn.f16x2.e2m1x2 %2, c;\n cvt.rn.f16x2.e2m1x2 %3, d;\n}\n" : "=r"(h[0]), "=r"(h[1]), "=r"(h[2]), "=r"(h[3]) : "r"(codes));
+        const uint64_t s2 = f2_pack(s, s), t2 = f2_pack(f.t, f.t);
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const uint32_t c = (codes >> (4 * i)) & 15u;
-            v[i] = __fmul_rn(e2m1_value(c, s), t);
+        for (int i = 0; i < N / 2; ++i) {
+            const float2 g = __half22float2(*reinterpret_cast<const __half2*>(&h[i]));
+            f2_unpack(f2_mul(f2_mul(f2_pack(g.x, g.y), s2), t2), v[2 * i], v[2 * i + 1]);
         }
         *stored = Vec<T>::pack(v);
     }
@@ -133,11 +169,11 @@ struct QuantArgs {
 // Pieces of 16 bytes: piece i of the call is piece i % ppr of row i / ppr.  A block takes PER x THREADS consecutive ones, all loads of a
 // thread in flight at once.
 template <typename T, int FMT, int PER>
-__global__ void __launch_bounds__(THREADS) quantize_kernel(QuantArgs a) {
+__global__ void __launch_bounds__(THREADS) quantize_kernel(const __grid_constant__ QuantArgs a) {
     KERNEL_PROLOGUE(20);   // fp4 quantize_kernel
     constexpr int N = Vec<T>::N, G = group(FMT);
     const int ppr = a.d / N, groups = a.d / G, g4 = (groups + 3) >> 2;
-    const float t = a.t ? __ldg(a.t) : 1.f;
+    const Factor t = make_factor<FMT>(a.t);
     const long long first = (long long)blockIdx.x * (PER * THREADS), total = a.rows * ppr;
     const long long row0 = first / ppr;
     const unsigned rem0 = (unsigned)(first - row0 * ppr);
@@ -194,7 +230,7 @@ constexpr int APPEND_MAX_ROWS = 64;              // rows of a block
 // blockIdx: x = rows_per_block rows, y = sequence, z = K or V.  A row that lists a position outside the cache is skipped, and so is one whose
 // position a later row lists again: the last one listed stays, whole.
 template <typename T>
-__global__ void __launch_bounds__(THREADS) kv_append_kernel(AppendArgs a) {
+__global__ void __launch_bounds__(THREADS) kv_append_kernel(const __grid_constant__ AppendArgs a) {
     KERNEL_PROLOGUE(21);   // fp4 kv_append_kernel
     constexpr int N = Vec<T>::N;
     __shared__ int pos[APPEND_MAX_ROWS];
@@ -212,8 +248,11 @@ __global__ void __launch_bounds__(THREADS) kv_append_kernel(AppendArgs a) {
         const int p = idx ? idx[r0 + i] : r0 + i;
         pos[i] = p >= 0 && p < a.cap ? p : -1;
     }
-    __syncthreads();
-    if (idx) {
+    // an ascending rest of the list, as a selection writes it, has nothing twice; any other is compared entry by entry
+    bool ascending = true;
+    if (idx)
+        for (int j = r0 + 1 + threadIdx.x; j < count; j += THREADS) ascending = ascending && __ldg(idx + j) > __ldg(idx + j - 1);
+    if (!__syncthreads_and(ascending)) {
         for (int j = r0 + 1 + threadIdx.x; j < count; j += THREADS) {
             const int p = __ldg(idx + j);
             for (int i = 0; i < min(live, j - r0); ++i)
@@ -222,7 +261,7 @@ __global__ void __launch_bounds__(THREADS) kv_append_kernel(AppendArgs a) {
         __syncthreads();
     }
     const int ppr = a.width / N, total = live * ppr;
-    const float t = a.t[which] ? __ldg(a.t[which]) : 1.f;
+    const Factor t = make_factor<NV>(a.t[which]);
     const uint4* x = reinterpret_cast<const uint4*>((const T*)a.x[which] + (seq * a.R + r0) * a.width);
     uint4* deq = a.deq[which] ? reinterpret_cast<uint4*>((T*)a.deq[which] + (seq * a.R + r0) * a.width) : nullptr;
     uint8_t* codes = a.codes[which] + seq * a.cap * (size_t)(a.width >> 1);

@@ -11,8 +11,6 @@
 namespace ps {
 namespace fp4 {
 
-using namespace tc;
-
 constexpr int KB = 256;                          // K of a ring slot: one 128-byte row of codes
 constexpr uint32_t BLOCK_BYTES = 512;            // scales of 128 rows x 4 groups
 __host__ __device__ constexpr int scale_blocks(int fmt) { return KB / (4 * group(fmt)); }       // per slot and 128 rows: 4 or 2
