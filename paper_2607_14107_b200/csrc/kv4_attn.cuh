@@ -32,7 +32,8 @@ struct Args {
     const uint8_t* kc; const uint8_t* ks; const uint8_t* vc; const uint8_t* vs;
     const float* tk; const float* tv;
     const int* lens;                             // [batch] keys of every sequence (null: cap)
-    float* part_o; float2* part_ml;              // partial rows: [split][batch * R * n_heads][DH], (maximum, sum)
+    float* part_o; float2* part_ml;              // partial rows: [part][batch * R * n_heads][DH], (maximum, sum)
+    int* part_n;                                 // [batch] parts of every sequence (tensor-core kernel; null: rows are written at once, or `split` parts)
     int R, cap, n_heads, n_kv, split;
     int part_keys;                               // keys of a part in the warp-level kernel
     long long rows_total;                        // batch * R * n_heads
@@ -385,12 +386,13 @@ __global__ void __launch_bounds__(JOIN_THREADS) kv4_attn_join_kernel(const __gri
     const int lane = threadIdx.x & 31;
     const long long row = (long long)blockIdx.x * (JOIN_THREADS / 32) + (threadIdx.x >> 5);
     if (row >= a.rows_total) return;
+    const int parts = a.part_n ? __ldcg(a.part_n + row / ((long long)a.R * a.n_heads)) : a.split;
     float2 ml[MAX_SPLIT / 32];
     float mm = -INFINITY;
 #pragma unroll
     for (int i = 0; i < MAX_SPLIT / 32; ++i) {
         const int p = i * 32 + lane;
-        ml[i] = p < a.split ? __ldcg(a.part_ml + (size_t)p * a.rows_total + row) : make_float2(-INFINITY, 0.f);
+        ml[i] = p < parts ? __ldcg(a.part_ml + (size_t)p * a.rows_total + row) : make_float2(-INFINITY, 0.f);
         mm = fmaxf(mm, ml[i].x);
     }
     mm = warp_max(mm);
@@ -404,7 +406,7 @@ __global__ void __launch_bounds__(JOIN_THREADS) kv4_attn_join_kernel(const __gri
     float acc[PER];
 #pragma unroll
     for (int c = 0; c < PER; ++c) acc[c] = 0.f;
-    for (int p0 = 0; p0 < a.split; p0 += 8) {    // eight parts' loads in flight
+    for (int p0 = 0; p0 < parts; p0 += 8) {    // eight parts' loads in flight
         float f[8];
         float2 x[8][PER / 2];
 #pragma unroll

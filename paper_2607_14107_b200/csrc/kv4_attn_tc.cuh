@@ -8,7 +8,8 @@
 //            16 conversions, 16 products and four 16-byte stores for every 32 channels
 //   scores   S = Q K^T in tensor memory; four warps per stream, one thread per row, keep a running maximum m and sum and write p = 2^(s - m + LIFT),
 //            rounded to fp16, over the scores, where it is the A operand of O += P V.  m moves only when it has been outgrown by 2^SLACK
-//   split    a grid of few row tiles splits the keys over CTAs; kv4_attn_join_kernel puts the parts together
+//   split    the key tiles of a batch are cut into parts of one length, the shortest that gives no more parts than there are CTAs, so that ragged
+//            lengths leave none of them idle; kv4_attn_join_kernel puts a sequence's parts together
 //
 // fp16 on both sides: keys and values are exact in it, q (bf16) is after a power of two per row, and probabilities keep three more bits than in bf16.
 // The method of the two streams and the lagging maximum is that of attn_flash.cuh (published; named there).  Every mbarrier wait is bounded.
@@ -33,11 +34,130 @@ static_assert(TC_MMA_REGS + 2 * TC_SOFTMAX_REGS + TC_CODE_REGS <= 4 * TC_LAUNCH_
 constexpr size_t TC_SMEM = 1024 + (2 + TC_SLOTS) * (size_t)TC_TILE + 4 * TC_DEPTH * RAW_BYTES;
 static_assert(TC_SMEM <= 227 * 1024, "shared memory");
 
+constexpr int TC_MAX_BATCH = 32;                 // sequences whose parts are cut to measure (a lane each)
 struct TcArgs {
     Args a;
-    int tiles;                                   // CTAs per K/V head: row tiles (key split) or pairs of them
+    int batch;
+    int tiles;                                   // CTAs per K/V head and part: row tiles (key split) or pairs of them
     int key_split;
+    int slots;                                   // parts per row tile and K/V head: batch <= TC_MAX_BATCH: at most, of equal length; else a.split for each sequence
 };
+
+// The part that slot number `slot` works on: sequence b, its part p of cnt, key tiles [t0, t0 + n).  False: more slots than parts.
+__device__ __forceinline__ bool find_part(const TcArgs& f, int slot, int& b, int& p, int& cnt, int& t0, int& n, int& len) {
+    const int lane = threadIdx.x & 31;
+    if (f.batch > TC_MAX_BATCH) {
+        b = slot / f.a.split; p = slot - b * f.a.split; cnt = f.a.split;
+        len = seq_len(f.a, b);
+        const int all = (len + TC_KEYS - 1) / TC_KEYS;
+        t0 = (int)((long long)all * p / cnt);
+        n = (int)((long long)all * (p + 1) / cnt) - t0;
+        return true;
+    }
+    const int my_len = lane < f.batch ? seq_len(f.a, lane) : 0, my = (my_len + TC_KEYS - 1) / TC_KEYS;
+    auto parts = [&](int size) { return lane < f.batch ? max(1, (my + size - 1) / size) : 0; };
+    int lo = 1, hi = max(1, __reduce_max_sync(0xffffffffu, my));          // (hi: a part for each sequence, which fits)
+    while (lo < hi) {
+        const int mid = (lo + hi) >> 1;
+        if (__reduce_add_sync(0xffffffffu, parts(mid)) <= f.slots) hi = mid; else lo = mid + 1;
+    }
+    const int mine = parts(lo);
+    int end = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) { const int x = __shfl_up_sync(0xffffffffu, end, o); if (lane >= o) end += x; }
+    const unsigned hit = __ballot_sync(0xffffffffu, slot >= end - mine && slot < end);
+    if (hit == 0) return false;
+    b = __ffs(hit) - 1;
+    p = slot - __shfl_sync(0xffffffffu, end - mine, b);
+    cnt = __shfl_sync(0xffffffffu, mine, b);
+    len = __shfl_sync(0xffffffffu, my_len, b);
+    t0 = p * lo;
+    n = min(lo, __shfl_sync(0xffffffffu, my, b) - t0);
+    return true;
+}
+
+// ---- codes -> operand tiles ---------------------------------------------------------------------------------------------
+// A part's tiles in the order the tensor core takes them, two units (K and V) per key tile: K_0, V_0, K_1, V_1, ..., or, two key tiles in flight, K_0,
+// K_1, V_0, K_2, V_1, K_3, ..., V_{n-2}, V_{n-1}.
+struct Units {
+    int n, t0, len, two;                         // key tiles, the first one, the sequence's keys, order
+    __device__ __forceinline__ int tile(int u, bool& is_v) const {
+        if (!two || n == 1) { is_v = (u & 1) != 0; return u >> 1; }
+        if (u < 2) { is_v = false; return u; }
+        const int w = u - 2;
+        if (w < 2 * (n - 2)) { is_v = (w & 1) == 0; return is_v ? w >> 1 : (w >> 1) + 2; }
+        is_v = true;
+        return n - 2 + (w - 2 * (n - 2));
+    }
+};
+// One warp's share: keys cw * 32 .. of units first, first + step, ...  It copies codes and scales DEPTH - 1 of them ahead into its staging ring at raw0
+// and arrives on full0 + 8 slot once its rows are in the unit's slot of the operand ring at ring0, whose release it waits for on free0 + 8 slot.
+// A row's 64 bytes of codes lie as four pieces, piece p at row * 64 + ((p ^ (row / 2 & 3)) << 4): the lanes that read one piece of eight rows then
+// spread over all banks.  Rows from the sequence's end on are filled with zeros and not read.
+template <int SLOTS, int DEPTH>
+__device__ __forceinline__ void turn_codes(const Args& a, const Units& un, int b, int kvh, int cw, int first, int step, uint32_t raw0, uint32_t ring0,
+                                           uint32_t full0, uint32_t free0, volatile int* abort_flag) {
+    const int lane = threadIdx.x & 31, r8 = lane & 7, piece = lane >> 3, units = 2 * un.n;
+    const size_t row0 = (size_t)b * a.cap, stride_c = (size_t)a.n_kv * 64, stride_s = (size_t)a.n_kv * 8;
+    auto fetch = [&](int i) {                    // this warp's piece of work number i
+        const int u = first + i * step;
+        if (u < units) {
+            bool is_v;
+            const int j0 = (un.t0 + un.tile(u, is_v)) * TC_KEYS + cw * 32;
+            const uint8_t* codes = (is_v ? a.vc : a.kc) + kvh * 64;
+            const uint8_t* scales = (is_v ? a.vs : a.ks) + kvh * 8;
+            const uint32_t dst = raw0 + (uint32_t)(i % DEPTH) * RAW_BYTES;
+#pragma unroll
+            for (int it = 0; it < 4; ++it) {
+                const int row = 8 * it + (lane >> 2), p = lane & 3, j = j0 + row;
+                const uint8_t* src = codes + (row0 + (j < un.len ? j : 0)) * stride_c + p * 16;
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst + (uint32_t)(row * 64 + ((p ^ ((row >> 1) & 3)) << 4))), "l"(src), "r"(j < un.len ? 16 : 0) : "memory");
+            }
+            const int j = j0 + lane;
+            const uint8_t* src = scales + (row0 + (j < un.len ? j : 0)) * stride_s;
+            asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"(dst + CODE_BYTES + (uint32_t)lane * 8u), "l"(src), "r"(j < un.len ? 8 : 0) : "memory");
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+#pragma unroll
+    for (int i = 0; i < DEPTH - 1; ++i) fetch(i);
+    bool ok = true;
+    Ring r(first, SLOTS);
+    for (int i = 0, u = first; u < units; ++i, u += step) {
+        __syncwarp();              // (every lane has read the staging area that is filled next)
+        fetch(i + DEPTH - 1);
+        asm volatile("cp.async.wait_group %0;" ::"n"(DEPTH - 1) : "memory");
+        __syncwarp();
+        if (u >= SLOTS) ok = mbar_wait(free0 + 8u * (uint32_t)r.slot, r.phase ^ 1u, abort_flag);
+        ok = __all_sync(0xffffffffu, ok) != 0;
+        if (!ok) break;
+        const uint32_t raw = raw0 + (uint32_t)(i % DEPTH) * RAW_BYTES;
+        const uint32_t dst = ring0 + (uint32_t)r.slot * TC_TILE + (uint32_t)(piece >> 1) * HALF_TILE + (uint32_t)(cw * 32) * 128u;
+#pragma unroll
+        for (int it = 0; it < 4; ++it) {
+            const int row = 8 * it + r8;
+            uint32_t w[4], sc;
+            asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3])
+                         : "r"(raw + (uint32_t)(row * 64 + ((piece ^ ((row >> 1) & 3)) << 4))) : "memory");
+            asm volatile("{\n .reg .u16 h;\n ld.shared.u16 h, [%1];\n cvt.u32.u16 %0, h;\n}\n" : "=r"(sc) : "r"(raw + CODE_BYTES + (uint32_t)(row * 8 + piece * 2)) : "memory");
+            const uint32_t sp = scales_to_half(sc), s0 = __byte_perm(sp, 0, 0x1010), s1 = __byte_perm(sp, 0, 0x3232);
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                uint32_t h[4];
+                codes_to_half(w[c], h);
+#pragma unroll
+                for (int x = 0; x < 4; ++x) h[x] = h2mul(h[x], c < 2 ? s0 : s1);
+                asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(dst + (uint32_t)row * 128u + (uint32_t)((((piece & 1) * 4 + c) ^ r8) << 4)),
+                             "r"(h[0]), "r"(h[1]), "r"(h[2]), "r"(h[3]) : "memory");
+            }
+        }
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncwarp();
+        if (lane == 0) mbar_arrive(full0 + 8u * (uint32_t)r.slot);
+        for (int x = 0; x < step; ++x) r.next(SLOTS);
+    }
+    asm volatile("cp.async.wait_all;" ::: "memory");
+}
 
 // fp16 x fp16 -> fp32, both operands K-major
 __device__ __forceinline__ uint32_t instr_desc_f16(int m, int n) { return (1u << 4) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(m >> 4) << 24); }
@@ -50,7 +170,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) kv4_attn_tc_kernel(const __grid
     __shared__ int abort_sh;
     const Args& a = f.a;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int tile = (int)blockIdx.x / a.split, part = (int)blockIdx.x - tile * a.split, kvh = blockIdx.y, b = blockIdx.z;
+    const int tile = (int)blockIdx.x / f.slots, slot_no = (int)blockIdx.x - tile * f.slots, kvh = blockIdx.y;
     const int hpg = a.n_heads / a.n_kv;
     const long long vrows = (long long)hpg * a.R;
     const bool ksplit = f.key_split != 0;
@@ -84,16 +204,15 @@ __global__ void __launch_bounds__(TC_THREADS, 1) kv4_attn_tc_kernel(const __grid
     pdl_wait();            // lengths, codes and q may all come from the kernel before
     const uint32_t tmem_base = tmem_base_sh;
 
-    // key tiles of this CTA: [t0, t0 + n) of the sequence's
-    const int len = seq_len(a, b);
-    const int tiles_all = (len + TC_KEYS - 1) / TC_KEYS;
-    const int t0 = (int)((long long)tiles_all * part / a.split), n = (int)((long long)tiles_all * (part + 1) / a.split) - t0;
+    int b = 0, part = 0, parts = 0, t0 = 0, n = 0, len = 0;
+    const bool busy = find_part(f, slot_no, b, part, parts, t0, n, len);
+    if (busy && a.part_n && part == 0 && tile == 0 && kvh == 0 && threadIdx.x == 0) a.part_n[b] = parts;
     const int cnt0 = ksplit ? (n + 1) >> 1 : n;                    // of stream 0 ...
     const int cnt1 = ksplit ? n >> 1 : (vr0 + TC_ROWS < vrows ? n : 0);       // ... and of stream 1
 
     if (warp < 4) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(TC_MMA_REGS));
-        if (warp == 0 && elect_one()) {
+        if (busy && warp == 0 && elect_one()) {
             const uint32_t idesc_s = instr_desc_f16(TC_ROWS, TC_KEYS);
             const uint32_t idesc_o = instr_desc_f16(TC_ROWS, TC_DH) | (1u << 16);       // B (= V) is MN-major
             bool ok = mbar_wait(bar_q, 0, abort_flag);
@@ -157,80 +276,13 @@ __global__ void __launch_bounds__(TC_THREADS, 1) kv4_attn_tc_kernel(const __grid
         }
     } else if (warp >= 12) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(TC_CODE_REGS));
-        // ---- codes -> operand tiles, in the order the tensor core takes them: row split K_0, V_0, K_1, V_1, ...; key split K_0, K_1, V_0, K_2,
-        // V_1, K_3, ..., V_{n-2}, V_{n-1}
-        const int cw = warp - 12, r8 = lane & 7, piece = lane >> 3;
-        const uint32_t raw0 = smem_base + (2 + TC_SLOTS) * TC_TILE + (uint32_t)cw * (TC_DEPTH * RAW_BYTES);
-        const size_t row0 = (size_t)b * a.cap;
-        const size_t stride_c = (size_t)a.n_kv * 64, stride_s = (size_t)a.n_kv * 8;
-        auto unit_tile = [&](int u, bool& is_v) {
-            if (!ksplit || n == 1) { is_v = (u & 1) != 0; return u >> 1; }
-            if (u < 2) { is_v = false; return u; }
-            const int w = u - 2;
-            if (w < 2 * (n - 2)) { is_v = (w & 1) == 0; return is_v ? w >> 1 : (w >> 1) + 2; }
-            is_v = true;
-            return n - 2 + (w - 2 * (n - 2));
-        };
-        // A row's 64 bytes of codes as four pieces, piece p at row * 64 + ((p ^ (row / 2 & 3)) << 4): the lanes that read one piece of eight rows then
-        // spread over all banks.  Rows from the sequence's end on are filled with zeros and not read.
-        auto fetch = [&](int u) {
-            if (u < 2 * n) {
-                bool is_v;
-                const int j0 = (t0 + unit_tile(u, is_v)) * TC_KEYS + cw * 32;
-                const uint8_t* codes = (is_v ? a.vc : a.kc) + kvh * 64;
-                const uint8_t* scales = (is_v ? a.vs : a.ks) + kvh * 8;
-                const uint32_t dst = raw0 + (uint32_t)(u % TC_DEPTH) * RAW_BYTES;
-#pragma unroll
-                for (int it = 0; it < 4; ++it) {
-                    const int row = 8 * it + (lane >> 2), p = lane & 3, j = j0 + row;
-                    const uint8_t* src = codes + (row0 + (j < len ? j : 0)) * stride_c + p * 16;
-                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst + (uint32_t)(row * 64 + ((p ^ ((row >> 1) & 3)) << 4))), "l"(src), "r"(j < len ? 16 : 0) : "memory");
-                }
-                const int j = j0 + lane;
-                const uint8_t* src = scales + (row0 + (j < len ? j : 0)) * stride_s;
-                asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"(dst + CODE_BYTES + (uint32_t)lane * 8u), "l"(src), "r"(j < len ? 8 : 0) : "memory");
-            }
-            asm volatile("cp.async.commit_group;" ::: "memory");
-        };
-        for (int u = 0; u < TC_DEPTH - 1; ++u) fetch(u);
-        bool ok = true;
-        Ring r(0, TC_SLOTS);
-        for (int u = 0; u < 2 * n; ++u, r.next(TC_SLOTS)) {
-            __syncwarp();          // (every lane has read the staging area that is filled next)
-            fetch(u + TC_DEPTH - 1);
-            asm volatile("cp.async.wait_group %0;" ::"n"(TC_DEPTH - 1) : "memory");
-            __syncwarp();
-            if (u >= TC_SLOTS) ok = mbar_wait(bar_free(r.slot), r.phase ^ 1u, abort_flag);
-            ok = __all_sync(0xffffffffu, ok) != 0;
-            if (!ok) break;
-            const uint32_t raw = raw0 + (uint32_t)(u % TC_DEPTH) * RAW_BYTES;
-            const uint32_t dst = ring_s(r.slot) + (uint32_t)(piece >> 1) * HALF_TILE + (uint32_t)(cw * 32) * 128u;
-#pragma unroll
-            for (int it = 0; it < 4; ++it) {
-                const int row = 8 * it + r8;
-                uint32_t w[4], sc;
-                asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3])
-                             : "r"(raw + (uint32_t)(row * 64 + ((piece ^ ((row >> 1) & 3)) << 4))) : "memory");
-                asm volatile("{\n .reg .u16 h;\n ld.shared.u16 h, [%1];\n cvt.u32.u16 %0, h;\n}\n" : "=r"(sc) : "r"(raw + CODE_BYTES + (uint32_t)(row * 8 + piece * 2)) : "memory");
-                const uint32_t sp = scales_to_half(sc), s0 = __byte_perm(sp, 0, 0x1010), s1 = __byte_perm(sp, 0, 0x3232);
-#pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                    uint32_t h[4];
-                    codes_to_half(w[c], h);
-#pragma unroll
-                    for (int x = 0; x < 4; ++x) h[x] = h2mul(h[x], c < 2 ? s0 : s1);
-                    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(dst + (uint32_t)row * 128u + (uint32_t)((((piece & 1) * 4 + c) ^ r8) << 4)),
-                                 "r"(h[0]), "r"(h[1]), "r"(h[2]), "r"(h[3]) : "memory");
-                }
-            }
-            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-            __syncwarp();
-            if (lane == 0) mbar_arrive(bar_full(r.slot));
-        }
-        asm volatile("cp.async.wait_all;" ::: "memory");
+        const Units un = {n, t0, len, ksplit};
+        if (busy) turn_codes<TC_SLOTS, TC_DEPTH>(a, un, b, kvh, warp - 12, 0, 1, smem_base + (2 + TC_SLOTS) * TC_TILE + (uint32_t)(warp - 12) * (TC_DEPTH * RAW_BYTES),
+                                                 ring_s(0), bar_full(0), bar_free(0), abort_flag);
     } else {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(TC_SOFTMAX_REGS));
         // ---- softmax warps: tensor-memory lane = row ----
+        if (busy) {
         const int sw = warp - 4, g = sw >> 2, quarter = warp & 3;
         const int row = quarter * 32 + lane;
         const int cnt = g ? cnt1 : cnt0;
@@ -373,10 +425,10 @@ __global__ void __launch_bounds__(TC_THREADS, 1) kv4_attn_tc_kernel(const __grid
             const size_t ro = q_row(vr);
             const float inv = none ? 0.f : tv / l;
             if ((g == 0 || !ksplit)) {
-                if (a.split > 1) a.part_ml[(size_t)part * a.rows_total + ro] = make_float2(m, ok ? l : __uint_as_float(0x7fc00000u));
+                if (a.part_n) a.part_ml[(size_t)part * a.rows_total + ro] = make_float2(m, ok ? l : __uint_as_float(0x7fc00000u));
                 else if (a.lse) a.lse[ro] = !ok ? __uint_as_float(0x7fc00000u) : none ? -INFINITY : (m - LIFT + log2f(l)) * 0.6931471805599453f;
             }
-            w0 *= a.split > 1 ? 1.f : inv; w1 *= a.split > 1 ? 1.f : inv;
+            w0 *= a.part_n ? 1.f : inv; w1 *= a.part_n ? 1.f : inv;
         }
         const int c_lo = ksplit ? 64 * g : 0, c_hi = (cnt > 0 || ksplit || n == 0) ? (ksplit ? c_lo + 64 : TC_DH) : 0;
         const uint32_t tO0 = tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(2 * TC_KEYS);
@@ -398,7 +450,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) kv4_attn_tc_kernel(const __grid
                 for (int i = 0; i < 32; ++i) o[i] = ok ? 0u : 0x7fc00000u;
             }
             if (vr < vrows) {
-                if (a.split > 1) {
+                if (a.part_n) {
                     float* dst = a.part_o + ((size_t)part * a.rows_total + q_row(vr)) * TC_DH + c;
 #pragma unroll
                     for (int q = 0; q < 8; ++q) *reinterpret_cast<uint4*>(dst + 4 * q) = make_uint4(o[4 * q], o[4 * q + 1], o[4 * q + 2], o[4 * q + 3]);
@@ -411,6 +463,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) kv4_attn_tc_kernel(const __grid
                     store16<__nv_bfloat16>(dst + 16, v + 16);
                 }
             }
+        }
         }
     }
     tc_fence_before();

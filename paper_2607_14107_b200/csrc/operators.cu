@@ -249,6 +249,7 @@ extern "C" int polestar_k_kv4_append(const void* k, const void* v, const int32_t
     return POLESTAR_OK;
 }
 
+constexpr size_t KV4_PARTS_BYTES = 65536 * sizeof(int);       // front of the scratch: parts of every sequence
 // Plans of the attention kernels: functions of the sizes alone, so that a scratch of polestar_k_kv4_scratch_bytes() bytes suffices for every call of
 // these sizes.  The warp-level kernel: tiles of 8 or 16 rows, parts of a fixed number of keys (those behind a short sequence's end leave at once).
 struct Kv4Warp { int tiles, rows, part_keys, split; };
@@ -265,21 +266,29 @@ static Kv4Warp kv4_warp_plan(long long batch, long long R, int cap, int n_heads,
     p.split = (cap + p.part_keys - 1) / p.part_keys;
     return p;
 }
-// The same for the tensor-core kernel: row tiles of 128 (one of them: split between the streams of a CTA) or pairs of them, one CTA per SM.  The
-// number of parts that needs the fewest waves of key tiles, a part being no shorter than four tiles.
-struct Kv4Tc { int tiles, key_split, split; };
+// The tensor-core kernel: row tiles of 128 (one of them: split between the streams of a CTA) or pairs of them, one CTA per SM.  Parts of the keys: the
+// number of waves of CTAs that costs the fewest key tiles (two tiles' worth of start and end, one and a half more where parts have to be joined), a part
+// of a sequence that fills the cache being no shorter than four tiles.
+struct Kv4Tc { int tiles, key_split, slots, split, parts; };
 static Kv4Tc kv4_tc_plan(long long batch, long long R, int cap, int n_heads, int n_kv) {
-    const long long row_tiles = (R * (n_heads / n_kv) + kv4::TC_ROWS - 1) / kv4::TC_ROWS;
+    const long long vrows = R * (n_heads / n_kv), row_tiles = (vrows + kv4::TC_ROWS - 1) / kv4::TC_ROWS;
     Kv4Tc p;
     p.key_split = row_tiles == 1;
     p.tiles = (int)((row_tiles + 1) / 2);
-    const long long base = batch * n_kv * p.tiles, key_tiles = (cap + kv4::TC_KEYS - 1) / kv4::TC_KEYS;
-    p.split = 1;
-    double best = 1e30;
-    for (int s = 1; s <= kv4::MAX_SPLIT && (s == 1 || key_tiles / s >= 4); ++s) {
-        const double cost = (double)((base * s + 147) / 148) * (double)((key_tiles + s - 1) / s + 2);       // two tiles' worth of start and end
-        if (cost < 0.97 * best) { best = cost; p.split = s; }
+    const long long per = (long long)n_kv * p.tiles, key_tiles = (cap + kv4::TC_KEYS - 1) / kv4::TC_KEYS;
+    long long slots = batch;
+    double best = (double)((per * batch + 147) / 148) * (double)(key_tiles + 2);
+    for (int w = 1; w <= 8; ++w) {
+        const long long s = std::min(148LL * w / per, batch * key_tiles / 4), c = s / batch;
+        if (c < 2) continue;
+        const double cost = w * ((double)((key_tiles + c - 1) / c) + 3.5);
+        if (cost < 0.97 * best) { best = cost; slots = s; }
     }
+    slots = std::min(slots, batch - 1 + kv4::MAX_SPLIT);
+    if (batch > kv4::TC_MAX_BATCH) slots = batch * std::min<long long>(kv4::MAX_SPLIT, slots / batch);      // the same number for every sequence
+    p.slots = (int)slots;
+    p.split = batch > kv4::TC_MAX_BATCH ? (int)(slots / batch) : 1;
+    p.parts = batch > kv4::TC_MAX_BATCH ? p.split : (int)(slots - batch + 1);       // at most, of one sequence
     return p;
 }
 static bool kv4_use_tc(int dtype, int head_dim, long long vrows) {
@@ -294,17 +303,18 @@ static bool kv4_attention_shape_ok(int batch, int R, int cap, int n_heads, int n
 extern "C" size_t polestar_k_kv4_scratch_bytes(int32_t batch, int32_t R, int32_t cap, int32_t n_heads, int32_t n_kv, int32_t head_dim) {
     if (!kv4_attention_shape_ok(batch, R, cap, n_heads, n_kv, head_dim)) return 0;
     const size_t rows = (size_t)batch * R * n_heads;
-    const int split = std::max(kv4_warp_plan(batch, R, cap, n_heads, n_kv).split, kv4_tc_plan(batch, R, cap, n_heads, n_kv).split);
-    return 256 + (split > 1 ? split * rows * ((size_t)head_dim * 4 + 8) : 0);
+    if (rows == 0) return 256;
+    const int split = std::max(kv4_warp_plan(batch, R, cap, n_heads, n_kv).split, kv4_tc_plan(batch, R, cap, n_heads, n_kv).parts);
+    return 256 + KV4_PARTS_BYTES + (split > 1 ? split * rows * ((size_t)head_dim * 4 + 8) : 0);
 }
 
 static dim3 join_grid(const kv4::Args& a) { return dim3((unsigned)((a.rows_total * 32 + kv4::JOIN_THREADS - 1) / kv4::JOIN_THREADS)); }
 static int launch_kv4_tc(const kv4::Args& a, const Kv4Tc& p, int batch, cudaStream_t st) {
     kv4::TcArgs f;
-    f.a = a; f.tiles = p.tiles; f.key_split = p.key_split;
-    if ((long long)p.tiles * a.split > INT32_MAX) return POLESTAR_E_INVAL;
-    CK(launch_k(kv4::kv4_attn_tc_kernel, dim3((unsigned)(p.tiles * a.split), a.n_kv, batch), dim3(kv4::TC_THREADS), kv4::TC_SMEM, st, f));
-    if (a.split > 1) CK(launch_k(kv4::kv4_attn_join_kernel<__nv_bfloat16, 128>, join_grid(a), dim3(kv4::JOIN_THREADS), 0, st, a));
+    f.a = a; f.batch = batch; f.tiles = p.tiles; f.key_split = p.key_split; f.slots = p.slots;
+    if ((long long)p.tiles * p.slots > INT32_MAX) return POLESTAR_E_INVAL;
+    CK(launch_k(kv4::kv4_attn_tc_kernel, dim3((unsigned)(p.tiles * p.slots), a.n_kv), dim3(kv4::TC_THREADS), kv4::TC_SMEM, st, f));
+    if (p.parts > 1) CK(launch_k(kv4::kv4_attn_join_kernel<__nv_bfloat16, 128>, join_grid(a), dim3(kv4::JOIN_THREADS), 0, st, a));
     return POLESTAR_OK;
 }
 template <typename T, int DH, int NB>
@@ -342,8 +352,9 @@ extern "C" int polestar_k_kv4_attention(const void* q, const uint8_t* kc, const 
     const Kv4Warp wplan = kv4_warp_plan(batch, R, cap, n_heads, n_kv);
     a.split = tc ? plan.split : wplan.split;
     a.part_keys = wplan.part_keys;
-    a.part_o = (float*)scratch;
-    a.part_ml = (float2*)((char*)scratch + (size_t)a.split * a.rows_total * head_dim * 4);
+    a.part_n = tc && plan.parts > 1 ? (int*)scratch : nullptr;
+    a.part_o = (float*)((char*)scratch + KV4_PARTS_BYTES);
+    a.part_ml = (float2*)((char*)a.part_o + (size_t)(tc ? plan.parts : wplan.split) * a.rows_total * head_dim * 4);
     a.scale = 1.0f / sqrtf((float)head_dim);
     cudaStream_t st = (cudaStream_t)stream;
     if (tc) return launch_kv4_tc(a, plan, batch, st);
