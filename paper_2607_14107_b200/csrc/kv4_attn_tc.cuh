@@ -98,24 +98,33 @@ template <int SLOTS, int DEPTH>
 __device__ __forceinline__ void turn_codes(const Args& a, const Units& un, int b, int kvh, int cw, int first, int step, uint32_t raw0, uint32_t ring0,
                                            uint32_t full0, uint32_t free0, volatile int* abort_flag) {
     const int lane = threadIdx.x & 31, r8 = lane & 7, piece = lane >> 3, units = 2 * un.n;
-    const size_t row0 = (size_t)b * a.cap, stride_c = (size_t)a.n_kv * 64, stride_s = (size_t)a.n_kv * 8;
+    const size_t stride_c = (size_t)a.n_kv * 64, stride_s = (size_t)a.n_kv * 8;
+    // what this lane copies of a unit: piece lane % 4 of rows lane / 4, + 8, + 16, + 24, and the scales of row `lane`
+    const size_t key0 = (size_t)b * a.cap + (size_t)un.t0 * TC_KEYS + cw * 32;
+    const size_t at_c = (key0 + (lane >> 2)) * stride_c + kvh * 64 + (lane & 3) * 16, at_s = (key0 + lane) * stride_s + kvh * 8;
+    const uint32_t to_c = (uint32_t)((lane >> 2) * 64 + (((lane & 3) ^ ((lane >> 3) & 3)) << 4)), to_s = CODE_BYTES + (uint32_t)lane * 8u;
+    const int left0 = un.len - un.t0 * TC_KEYS - cw * 32;                  // keys from this warp's first one on
     auto fetch = [&](int i) {                    // this warp's piece of work number i
         const int u = first + i * step;
         if (u < units) {
             bool is_v;
-            const int j0 = (un.t0 + un.tile(u, is_v)) * TC_KEYS + cw * 32;
-            const uint8_t* codes = (is_v ? a.vc : a.kc) + kvh * 64;
-            const uint8_t* scales = (is_v ? a.vs : a.ks) + kvh * 8;
+            const int t = un.tile(u, is_v), left = left0 - t * TC_KEYS;
+            const uint8_t* codes = (is_v ? a.vc : a.kc) + at_c + (size_t)t * (TC_KEYS * stride_c);
+            const uint8_t* scales = (is_v ? a.vs : a.ks) + at_s + (size_t)t * (TC_KEYS * stride_s);
             const uint32_t dst = raw0 + (uint32_t)(i % DEPTH) * RAW_BYTES;
+            if (left >= 32) {
 #pragma unroll
-            for (int it = 0; it < 4; ++it) {
-                const int row = 8 * it + (lane >> 2), p = lane & 3, j = j0 + row;
-                const uint8_t* src = codes + (row0 + (j < un.len ? j : 0)) * stride_c + p * 16;
-                asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst + (uint32_t)(row * 64 + ((p ^ ((row >> 1) & 3)) << 4))), "l"(src), "r"(j < un.len ? 16 : 0) : "memory");
+                for (int it = 0; it < 4; ++it)
+                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst + to_c + (uint32_t)(it * 512)), "l"(codes + (size_t)(8 * it) * stride_c) : "memory");
+                asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(dst + to_s), "l"(scales) : "memory");
+            } else {                             // rows from the end on: zeros, from an address that is not read
+#pragma unroll
+                for (int it = 0; it < 4; ++it) {
+                    const bool in = 8 * it + (lane >> 2) < left;
+                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst + to_c + (uint32_t)(it * 512)), "l"(in ? codes + (size_t)(8 * it) * stride_c : a.kc), "r"(in ? 16 : 0) : "memory");
+                }
+                asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"(dst + to_s), "l"(lane < left ? scales : a.ks), "r"(lane < left ? 8 : 0) : "memory");
             }
-            const int j = j0 + lane;
-            const uint8_t* src = scales + (row0 + (j < un.len ? j : 0)) * stride_s;
-            asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"(dst + CODE_BYTES + (uint32_t)lane * 8u), "l"(src), "r"(j < un.len ? 8 : 0) : "memory");
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
     };
@@ -133,21 +142,24 @@ __device__ __forceinline__ void turn_codes(const Args& a, const Units& un, int b
         if (!ok) break;
         const uint32_t raw = raw0 + (uint32_t)(i % DEPTH) * RAW_BYTES;
         const uint32_t dst = ring0 + (uint32_t)r.slot * TC_TILE + (uint32_t)(piece >> 1) * HALF_TILE + (uint32_t)(cw * 32) * 128u;
+        uint32_t w[4][4], sc[4];
 #pragma unroll
         for (int it = 0; it < 4; ++it) {
             const int row = 8 * it + r8;
-            uint32_t w[4], sc;
-            asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3])
+            asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w[it][0]), "=r"(w[it][1]), "=r"(w[it][2]), "=r"(w[it][3])
                          : "r"(raw + (uint32_t)(row * 64 + ((piece ^ ((row >> 1) & 3)) << 4))) : "memory");
-            asm volatile("{\n .reg .u16 h;\n ld.shared.u16 h, [%1];\n cvt.u32.u16 %0, h;\n}\n" : "=r"(sc) : "r"(raw + CODE_BYTES + (uint32_t)(row * 8 + piece * 2)) : "memory");
-            const uint32_t sp = scales_to_half(sc), s0 = __byte_perm(sp, 0, 0x1010), s1 = __byte_perm(sp, 0, 0x3232);
+            asm volatile("{\n .reg .u16 h;\n ld.shared.u16 h, [%1];\n cvt.u32.u16 %0, h;\n}\n" : "=r"(sc[it]) : "r"(raw + CODE_BYTES + (uint32_t)(row * 8 + piece * 2)) : "memory");
+        }
+#pragma unroll
+        for (int it = 0; it < 4; ++it) {
+            const uint32_t sp = scales_to_half(sc[it]), s0 = __byte_perm(sp, 0, 0x1010), s1 = __byte_perm(sp, 0, 0x3232);
 #pragma unroll
             for (int c = 0; c < 4; ++c) {
                 uint32_t h[4];
-                codes_to_half(w[c], h);
+                codes_to_half(w[it][c], h);
 #pragma unroll
                 for (int x = 0; x < 4; ++x) h[x] = h2mul(h[x], c < 2 ? s0 : s1);
-                asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(dst + (uint32_t)row * 128u + (uint32_t)((((piece & 1) * 4 + c) ^ r8) << 4)),
+                asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(dst + (uint32_t)((8 * it + r8) * 128) + (uint32_t)((((piece & 1) * 4 + c) ^ r8) << 4)),
                              "r"(h[0]), "r"(h[1]), "r"(h[2]), "r"(h[3]) : "memory");
             }
         }

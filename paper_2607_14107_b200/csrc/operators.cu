@@ -266,35 +266,48 @@ static Kv4Warp kv4_warp_plan(long long batch, long long R, int cap, int n_heads,
     p.split = (cap + p.part_keys - 1) / p.part_keys;
     return p;
 }
-// The tensor-core kernel: row tiles of 128 (one of them: split between the streams of a CTA) or pairs of them, one CTA per SM.  Parts of the keys: the
-// number of waves of CTAs that costs the fewest key tiles (two tiles' worth of start and end, one and a half more where parts have to be joined), a part
-// of a sequence that fills the cache being no shorter than four tiles.
-struct Kv4Tc { int tiles, key_split, slots, split, parts; };
+// The tensor-core kernel, one CTA per SM: row tiles of 128, one per CTA with its keys split between the streams, or two per CTA.  Two share the turning of
+// codes (a pair takes 2.5 us for 128 keys, one tile 2.1, one of up to 64 rows 1.4), one gives more CTAs where there are few.  Whichever needs less time, by those figures and
+// 8.5 us of start and end, with the keys cut into the number of parts that does (3 us more for joining them); a part of a sequence that fills the cache is
+// no shorter than four key tiles.
+struct Kv4Tc { int tiles, key_split, slots, split, parts; double us; };
 static Kv4Tc kv4_tc_plan(long long batch, long long R, int cap, int n_heads, int n_kv) {
-    const long long vrows = R * (n_heads / n_kv), row_tiles = (vrows + kv4::TC_ROWS - 1) / kv4::TC_ROWS;
+    const long long vrows = R * (n_heads / n_kv), row_tiles = (vrows + kv4::TC_ROWS - 1) / kv4::TC_ROWS, key_tiles = (cap + kv4::TC_KEYS - 1) / kv4::TC_KEYS;
     Kv4Tc p;
-    p.key_split = row_tiles == 1;
-    p.tiles = (int)((row_tiles + 1) / 2);
-    const long long per = (long long)n_kv * p.tiles, key_tiles = (cap + kv4::TC_KEYS - 1) / kv4::TC_KEYS;
-    long long slots = batch;
-    double best = (double)((per * batch + 147) / 148) * (double)(key_tiles + 2);
-    for (int w = 1; w <= 8; ++w) {
-        const long long s = std::min(148LL * w / per, batch * key_tiles / 4), c = s / batch;
-        if (c < 2) continue;
-        const double cost = w * ((double)((key_tiles + c - 1) / c) + 3.5);
-        if (cost < 0.97 * best) { best = cost; slots = s; }
+    p.us = 1e30;
+    for (int one = 1; one >= 0; --one) {
+        if (!one && row_tiles == 1) continue;
+        const long long tiles = one ? row_tiles : (row_tiles + 1) / 2, per = (long long)n_kv * tiles;
+        const double tile_us = !one ? 2.5 : vrows <= 64 ? 1.4 : 2.1;
+        for (int w = 0; w <= 8; ++w) {           // waves of CTAs; 0: a part for each sequence, whatever that takes
+            const long long s = w ? std::min(std::min(148LL * w / per, batch * key_tiles / 4), batch - 1 + kv4::MAX_SPLIT) : batch, c = s / batch;
+            if (w && c < 2) continue;
+            const double us = (w ? (double)w : (double)((per * batch + 147) / 148)) * (double)((key_tiles + c - 1) / c) * tile_us + 8.5 + (w ? 3.0 : 0.0);
+            if (us >= 0.97 * p.us) continue;
+            p.us = us; p.key_split = one; p.tiles = (int)tiles; p.slots = (int)s;
+        }
     }
-    slots = std::min(slots, batch - 1 + kv4::MAX_SPLIT);
-    if (batch > kv4::TC_MAX_BATCH) slots = batch * std::min<long long>(kv4::MAX_SPLIT, slots / batch);      // the same number for every sequence
-    p.slots = (int)slots;
-    p.split = batch > kv4::TC_MAX_BATCH ? (int)(slots / batch) : 1;
-    p.parts = batch > kv4::TC_MAX_BATCH ? p.split : (int)(slots - batch + 1);       // at most, of one sequence
+    const bool same = batch > kv4::TC_MAX_BATCH;                           // the same number of parts for every sequence
+    if (same) p.slots = (int)(batch * (p.slots / batch));
+    p.split = same ? (int)(p.slots / batch) : 1;
+    p.parts = same ? p.split : (int)(p.slots - batch + 1);                 // at most, of one sequence
     return p;
 }
-static bool kv4_use_tc(int dtype, int head_dim, long long vrows) {
+// Which kernel: the warp-level one turns codes again for every 16 rows, the tensor-core one once for 128 or 256, but it starts slowly and its rows fill whole
+// tiles.  The warp-level one's time as measured: 0.75 us for 16 rows x 128 keys on an SM, or, three CTAs per SM at a time, 1.4 us of latency for 128 keys of a
+// part while the CTAs have an SM for two of theirs, 3.2 us once they share them (2.4 in long parts), and 5 us (3 more for joining parts).  us, warp-level / tensor-core:
+// 7 rows a K/V head, eight ragged sequences of up to 32768 keys 39 / 71; 32 rows, 512 keys x 32 heads 10.5 / 12.8, 8 x 4096 keys x 32 heads 89 / 99; 48 rows,
+// 2 x 1500 keys x 32 heads 30 / 21; 64 rows, 8 x 2048 keys x 32 heads 84 / 58; 224 rows, 300 keys x 4 heads 8.4 / 13.4; 448 rows, 8 x 800 keys x 4
+// heads 40 / 19; 896 rows, 65536 keys x 4 heads 650 / 156.
+static bool kv4_use_tc(int dtype, int head_dim, const Kv4Warp& w, const Kv4Tc& t, long long batch, int cap, int n_kv) {
     if (dtype != POLESTAR_BF16 || head_dim != kv4::TC_DH) return false;
     const int forced = switch_kv4();
-    return forced ? forced == 2 : vrows > 16;
+    if (forced) return forced == 2;
+    const double ctas = (double)batch * n_kv * w.tiles * w.split, part = (double)((std::min(cap, w.part_keys) + 127) / 128);
+    const double all = (double)batch * n_kv * w.tiles * ((cap + 127) / 128);
+    double tile = 1.4 + 1.8 * std::min(1.0, std::max(0.0, (ctas - 74) / 100));
+    if (part >= 8) tile = std::min(tile, 2.4);
+    return t.us < std::max(all / 148 * 0.75, std::max(1.0, ctas / 444) * part * tile) + 5 + (w.split > 1 ? 3 : 0);
 }
 static bool kv4_attention_shape_ok(int batch, int R, int cap, int n_heads, int n_kv, int head_dim) {
     return kv4_shape_ok(batch, R, cap, n_kv, head_dim) && R <= 65536 && n_heads > 0 && n_heads <= 1024 && n_heads % n_kv == 0;
@@ -347,9 +360,9 @@ extern "C" int polestar_k_kv4_attention(const void* q, const uint8_t* kc, const 
     kv4::Args a;
     a.q = q; a.out = out; a.lse = lse; a.kc = kc; a.ks = ks; a.vc = vc; a.vs = vs; a.tk = k_scale; a.tv = v_scale; a.lens = lens;
     a.R = R; a.cap = cap; a.n_heads = n_heads; a.n_kv = n_kv; a.rows_total = (long long)batch * R * n_heads;
-    const bool tc = kv4_use_tc(dtype, head_dim, (long long)R * (n_heads / n_kv));
     const Kv4Tc plan = kv4_tc_plan(batch, R, cap, n_heads, n_kv);
     const Kv4Warp wplan = kv4_warp_plan(batch, R, cap, n_heads, n_kv);
+    const bool tc = kv4_use_tc(dtype, head_dim, wplan, plan, batch, cap, n_kv);
     a.split = tc ? plan.split : wplan.split;
     a.part_keys = wplan.part_keys;
     a.part_n = tc && plan.parts > 1 ? (int*)scratch : nullptr;
