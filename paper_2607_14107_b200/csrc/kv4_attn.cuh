@@ -22,8 +22,9 @@ namespace kv4 {
 constexpr int WARPS = 4, THREADS = WARPS * 32;
 constexpr int CHUNK = 16;                        // keys a warp takes at a time
 constexpr int DEPTH = 4;                         // chunks of a warp's ring
-constexpr int MAX_SPLIT = 64;
-constexpr int JOIN_THREADS = 64;
+constexpr int MAX_SPLIT = 128;
+constexpr int JOIN_THREADS = 128;
+constexpr int MAX_BATCH = 32;                    // sequences whose parts are cut to measure (a lane each)
 constexpr float SLACK = 8.f;                     // log2 of how far the running maximum may lag behind
 constexpr float LIFT = 7.f;                      // probabilities are 2^(s - m + LIFT): fp16 then keeps them down to 2^-31 of the largest
 
@@ -33,9 +34,9 @@ struct Args {
     const float* tk; const float* tv;
     const int* lens;                             // [batch] keys of every sequence (null: cap)
     float* part_o; float2* part_ml;              // partial rows: [part][batch * R * n_heads][DH], (maximum, sum)
-    int* part_n;                                 // [batch] parts of every sequence (tensor-core kernel; null: rows are written at once, or `split` parts)
-    int R, cap, n_heads, n_kv, split;
-    int part_keys;                               // keys of a part in the warp-level kernel
+    int* part_n;                                 // [batch] parts of every sequence (null: a part for each, rows are written at once)
+    int batch, R, cap, n_heads, n_kv;
+    int slots;                                   // parts per row tile and K/V head: up to MAX_BATCH sequences: at most, all of one length; beyond: the same number of each
     long long rows_total;                        // batch * R * n_heads
     float scale;
 };
@@ -68,6 +69,49 @@ __device__ __forceinline__ uint32_t pack_half(float lo, float hi) {
 __device__ __forceinline__ float2 unpack_half(uint32_t w) { return __half22float2(*reinterpret_cast<const __half2*>(&w)); }
 
 __device__ __forceinline__ int seq_len(const Args& a, int b) { return a.lens ? min(max(__ldg(a.lens + b), 0), a.cap) : a.cap; }
+// The part that slot number `slot` works on: sequence b with `len` keys, its part p, units of KEYS keys [t0, t0 + n).  False: there are more slots than parts.
+// `tell`: the thread that writes down how many parts a sequence has.  The whole warp calls.
+template <int KEYS>
+__device__ __forceinline__ bool find_part(const Args& a, int slot, bool tell, int& b, int& p, int& t0, int& n, int& len) {
+    const int lane = threadIdx.x & 31;
+    if (a.batch > MAX_BATCH || a.slots == a.batch) {
+        const int each = a.slots / a.batch;
+        b = slot / each; p = slot - b * each;
+        len = seq_len(a, b);
+        const int all = (len + KEYS - 1) / KEYS;
+        t0 = (int)((long long)all * p / each);
+        n = (int)((long long)all * (p + 1) / each) - t0;
+        if (tell && p == 0 && a.part_n) a.part_n[b] = each;
+        return true;
+    }
+    // the shortest length that gives no more parts than slots, an empty sequence having one too, and none more than MAX_SPLIT
+    const int my_len = lane < a.batch ? seq_len(a, lane) : 0, my = (my_len + KEYS - 1) / KEYS;
+    auto parts = [&](int size) { return lane < a.batch ? max(1, (my + size - 1) / size) : 0; };
+    const int longest = __reduce_max_sync(0xffffffffu, my);
+    int lo = max(max(1, ((int)__reduce_add_sync(0xffffffffu, my) + a.slots - 1) / a.slots), (longest + MAX_SPLIT - 1) / MAX_SPLIT), hi = max(lo, longest);
+    while (lo < hi) {
+        // (one sequence, or none that ends inside a part: the first length fits)
+        if ((int)__reduce_add_sync(0xffffffffu, parts(lo)) <= a.slots) break;
+        const int mid = (lo + 1 + hi) >> 1;
+        if ((int)__reduce_add_sync(0xffffffffu, parts(mid)) <= a.slots) hi = mid; else lo = mid;
+        if (lo + 1 >= hi) { lo = hi; break; }
+    }
+    const int mine = parts(lo);
+    int end = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) { const int x = __shfl_up_sync(0xffffffffu, end, o); if (lane >= o) end += x; }
+    const unsigned hit = __ballot_sync(0xffffffffu, slot >= end - mine && slot < end);
+    if (hit == 0) return false;
+    b = __ffs(hit) - 1;
+    p = slot - __shfl_sync(0xffffffffu, end - mine, b);
+    const int cnt = __shfl_sync(0xffffffffu, mine, b);
+    len = __shfl_sync(0xffffffffu, my_len, b);
+    t0 = p * lo;
+    n = min(lo, __shfl_sync(0xffffffffu, my, b) - t0);
+    if (tell && p == 0 && a.part_n) a.part_n[b] = cnt;
+    return true;
+}
+
 template <typename T> struct QPair;
 template <> struct QPair<float> { static __device__ __forceinline__ float2 load(const float* p) { return __ldg(reinterpret_cast<const float2*>(p)); } };
 template <> struct QPair<__nv_bfloat16> {
@@ -97,7 +141,7 @@ __device__ __forceinline__ uint32_t transpose8x8(uint32_t a) {
     return d;
 }
 
-// grid: x = tile of 8 NB rows x part of the keys, y = K/V head, z = sequence.  Lane (g = lane / 4, t = lane % 4).
+// grid: x = tile of 8 NB rows x part, y = K/V head.  Lane (g = lane / 4, t = lane % 4).
 // fp32 rows: q and the probabilities are each two fp16 terms (22 bits), with a product per term.
 template <typename T, int DH, int NB>
 __global__ void __launch_bounds__(THREADS) kv4_attn_warp_kernel(const __grid_constant__ Args a) {
@@ -107,21 +151,17 @@ __global__ void __launch_bounds__(THREADS) kv4_attn_warp_kernel(const __grid_con
     extern __shared__ uint8_t smem_raw[];
     __shared__ float sm[WARPS][ROWS], sl[WARPS][ROWS];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-    const int tile = (int)blockIdx.x / a.split, part = (int)blockIdx.x - tile * a.split, kvh = blockIdx.y, b = blockIdx.z;
+    const int tile = (int)blockIdx.x / a.slots, slot_no = (int)blockIdx.x - tile * a.slots, kvh = blockIdx.y;
     const int hpg = a.n_heads / a.n_kv;
     const long long vrows = (long long)hpg * a.R, vr0 = (long long)tile * ROWS;
-    const int len = seq_len(a, b);
-    const int lo = min(len, part * a.part_keys), hi = min(len, lo + a.part_keys);
+    constexpr int STEP = WARPS * CHUNK;
+    int b = 0, part = 0, t0 = 0, units = 0, len = 0;
+    if (!find_part<STEP>(a, slot_no, tile == 0 && kvh == 0 && threadIdx.x == 0, b, part, t0, units, len)) return;
+    const int lo = t0 * STEP, hi = min(len, lo + units * STEP);
     auto q_row = [&](long long vr) {             // virtual row -> row of [batch * R * n_heads]
         const int h = (int)(vr / a.R), r = (int)(vr - (long long)h * a.R);
         return ((size_t)b * a.R + r) * a.n_heads + kvh * hpg + h;
     };
-    if (lo >= hi && a.split > 1) {               // a part without keys: nothing but its empty sum
-        for (int i = threadIdx.x; i < ROWS; i += THREADS)
-            if (vr0 + i < vrows) a.part_ml[(size_t)part * a.rows_total + q_row(vr0 + i)] = make_float2(-INFINITY, 0.f);
-        return;
-    }
-
     // ---- the ring: what this lane copies of a chunk (sixteen-byte pieces of codes, the scales of one row) ----
     constexpr int PIECES = DH / 32, COPIES = CHUNK * PIECES / 32;          // of a row; per lane, keys and values each
     const uint32_t ring = (uint32_t)__cvta_generic_to_shared(smem_raw) + (uint32_t)warp * (DEPTH * St::BYTES);
@@ -130,23 +170,38 @@ __global__ void __launch_bounds__(THREADS) kv4_attn_warp_kernel(const __grid_con
     const uint8_t* fk = a.kc + (seq0 + fj) * row_c + kvh * (DH / 2);
     const uint8_t* fv = a.vc + (seq0 + fj) * row_c + kvh * (DH / 2);
     const uint8_t* fs = (lane < 16 ? a.ks : a.vs) + (seq0 + fj + (lane & 15)) * row_s + kvh * (DH / 16);
+    size_t off[COPIES];
+    uint32_t to_v[COPIES];
+#pragma unroll
+    for (int i = 0; i < COPIES; ++i) {
+        const int x = i * 32 + lane, r = x / PIECES, p = x % PIECES;
+        off[i] = (size_t)r * row_c + p * 16;
+        to_v[i] = St::V + St::v_piece(r, p);
+    }
     auto fetch = [&](int slot) {
         const uint32_t dst = ring + (uint32_t)slot * St::BYTES;
-        if (fj < hi) {
+        if (fj + CHUNK <= hi) {
 #pragma unroll
             for (int i = 0; i < COPIES; ++i) {
-                const int x = i * 32 + lane, r = x / PIECES, p = x % PIECES;
-                const uint32_t n = fj + r < hi ? 16u : 0u;                 // rows from the end on are zeros and not read
-                const size_t off = n ? (size_t)r * row_c + p * 16 : 0;
-                asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst + St::K + (uint32_t)(x * 16)), "l"(fk + off), "r"(n) : "memory");
-                asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst + St::V + St::v_piece(r, p)), "l"(fv + off), "r"(n) : "memory");
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst + St::K + (uint32_t)((i * 32 + lane) * 16)), "l"(fk + off[i]) : "memory");
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst + to_v[i]), "l"(fv + off[i]) : "memory");
+            }
+            if constexpr (DH == 128) asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(dst + St::KS + (uint32_t)lane * 8u), "l"(fs) : "memory");
+            else asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst + St::KS + (uint32_t)lane * 4u), "l"(fs) : "memory");
+            fj += WARPS * CHUNK;
+            fk += WARPS * CHUNK * row_c; fv += WARPS * CHUNK * row_c; fs += WARPS * CHUNK * row_s;
+        } else if (fj < hi) {                    // rows from the end on are zeros and not read
+#pragma unroll
+            for (int i = 0; i < COPIES; ++i) {
+                const bool in = fj + (i * 32 + lane) / PIECES < hi;
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst + St::K + (uint32_t)((i * 32 + lane) * 16)), "l"(in ? fk + off[i] : a.kc), "r"(in ? 16u : 0u) : "memory");
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst + to_v[i]), "l"(in ? fv + off[i] : a.kc), "r"(in ? 16u : 0u) : "memory");
             }
             const bool in = fj + (lane & 15) < hi;
             const uint8_t* src = in ? fs : a.ks;
             if constexpr (DH == 128) asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"(dst + St::KS + (uint32_t)lane * 8u), "l"(src), "r"(in ? 8u : 0u) : "memory");
             else asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst + St::KS + (uint32_t)lane * 4u), "l"(src), "r"(in ? 4u : 0u) : "memory");
-            fj += WARPS * CHUNK;
-            fk += WARPS * CHUNK * row_c; fv += WARPS * CHUNK * row_c; fs += WARPS * CHUNK * row_s;
+            fj = hi;
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
     };
@@ -194,9 +249,11 @@ __global__ void __launch_bounds__(THREADS) kv4_attn_warp_kernel(const __grid_con
     for (int i = 0; i < MT; ++i)
 #pragma unroll
         for (int n = 0; n < NB; ++n) o[i][n][0] = o[i][n][1] = o[i][n][2] = o[i][n][3] = 0.f;
-    float m[NB][2], l[NB][2];                    // l: this lane's keys only
+    float m[NB][2], most[NB][2], low[NB][2], l[NB][2];       // most = m + SLACK, low = m - LIFT (0 while m is -inf: p = 0 all the same), l: this lane's keys only
 #pragma unroll
-    for (int n = 0; n < NB; ++n) { m[n][0] = m[n][1] = -INFINITY; l[n][0] = l[n][1] = 0.f; }
+    for (int n = 0; n < NB; ++n)
+#pragma unroll
+        for (int x = 0; x < 2; ++x) { m[n][x] = most[n][x] = -INFINITY; low[n][x] = l[n][x] = 0.f; }
 
     int slot = 0;
     for (int j0 = lo + warp * CHUNK; j0 < hi; j0 += WARPS * CHUNK) {
@@ -216,10 +273,10 @@ __global__ void __launch_bounds__(THREADS) kv4_attn_warp_kernel(const __grid_con
                 const uint32_t row = (uint32_t)(g + 8 * i);
                 if constexpr (DH == 128) {
                     asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(kw[i][0]), "=r"(kw[i][1]), "=r"(kw[i][2]), "=r"(kw[i][3]) : "r"(st + St::K + row * 64u + (uint32_t)t * 16u) : "memory");
-                    asm volatile("{\n .reg .u16 h;\n ld.shared.u16 h, [%1];\n cvt.u32.u16 %0, h;\n}\n" : "=r"(ksc[i]) : "r"(st + St::KS + row * 8u + (uint32_t)t * 2u) : "memory");
+                    asm volatile("ld.shared.u16 %0, [%1];" : "=r"(ksc[i]) : "r"(st + St::KS + row * 8u + (uint32_t)t * 2u) : "memory");
                 } else {
                     asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(kw[i][0]), "=r"(kw[i][1]) : "r"(st + St::K + row * 32u + (uint32_t)t * 8u) : "memory");
-                    asm volatile("{\n .reg .u16 h;\n ld.shared.u8 h, [%1];\n cvt.u32.u16 %0, h;\n}\n" : "=r"(ksc[i]) : "r"(st + St::KS + row * 4u + (uint32_t)t) : "memory");
+                    asm volatile("ld.shared.u8 %0, [%1];" : "=r"(ksc[i]) : "r"(st + St::KS + row * 4u + (uint32_t)t) : "memory");
                     ksc[i] *= 0x101u;
                 }
             }
@@ -256,7 +313,7 @@ __global__ void __launch_bounds__(THREADS) kv4_attn_warp_kernel(const __grid_con
 #pragma unroll
             for (int x = 0; x < 2; ++x) {
                 top[n][x] = fmaxf(s[n][x], s[n][x + 2]);
-                grow |= top[n][x] > m[n][x] + SLACK;
+                grow |= top[n][x] > most[n][x];
             }
         }
         if (__any_sync(0xffffffffu, grow)) {
@@ -267,9 +324,11 @@ __global__ void __launch_bounds__(THREADS) kv4_attn_warp_kernel(const __grid_con
                     float nm = top[n][x];
 #pragma unroll
                     for (int d = 4; d < 32; d <<= 1) nm = fmaxf(nm, __shfl_xor_sync(0xffffffffu, nm, d));
-                    nm = nm > m[n][x] + SLACK ? nm : m[n][x];
+                    nm = nm > most[n][x] ? nm : m[n][x];
                     const float f = m[n][x] == -INFINITY ? 0.f : ex2(m[n][x] - nm);
                     m[n][x] = nm;
+                    most[n][x] = nm + SLACK;
+                    low[n][x] = nm == -INFINITY ? 0.f : nm - LIFT;
                     l[n][x] *= f;
 #pragma unroll
                     for (int i = 0; i < MT; ++i) { o[i][n][x] *= f; o[i][n][x + 2] *= f; }
@@ -280,10 +339,7 @@ __global__ void __launch_bounds__(THREADS) kv4_attn_warp_kernel(const __grid_con
         for (int n = 0; n < NB; ++n) {
             float p[4];
 #pragma unroll
-            for (int x = 0; x < 4; ++x) {
-                const float base = m[n][x & 1] == -INFINITY ? 0.f : m[n][x & 1] - LIFT;      // (nothing but -inf so far: p = 0)
-                p[x] = ex2(s[n][x] - base);
-            }
+            for (int x = 0; x < 4; ++x) p[x] = ex2(s[n][x] - low[n][x & 1]);
             l[n][0] += p[0] + p[2];
             l[n][1] += p[1] + p[3];
 #pragma unroll
@@ -303,10 +359,10 @@ __global__ void __launch_bounds__(THREADS) kv4_attn_warp_kernel(const __grid_con
             const int row = 2 * t + (i & 1) + 8 * (i >> 1);
             if constexpr (DH == 128) {
                 asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(vw[i][0]), "=r"(vw[i][1]) : "r"(st + St::V + St::v_piece(row, g >> 1) + (uint32_t)(g & 1) * 8u) : "memory");
-                asm volatile("{\n .reg .u16 h;\n ld.shared.u8 h, [%1];\n cvt.u32.u16 %0, h;\n}\n" : "=r"(vsc[i]) : "r"(st + St::VS + (uint32_t)(row * 8 + g)) : "memory");
+                asm volatile("ld.shared.u8 %0, [%1];" : "=r"(vsc[i]) : "r"(st + St::VS + (uint32_t)(row * 8 + g)) : "memory");
             } else {
                 asm volatile("ld.shared.b32 %0, [%1];" : "=r"(vw[i][0]) : "r"(st + St::V + (uint32_t)(row * 32 + g * 4)) : "memory");
-                asm volatile("{\n .reg .u16 h;\n ld.shared.u8 h, [%1];\n cvt.u32.u16 %0, h;\n}\n" : "=r"(vsc[i]) : "r"(st + St::VS + (uint32_t)(row * 4 + (g >> 1))) : "memory");
+                asm volatile("ld.shared.u8 %0, [%1];" : "=r"(vsc[i]) : "r"(st + St::VS + (uint32_t)(row * 4 + (g >> 1))) : "memory");
             }
         }
         const uint32_t vs0 = scales_to_half(vsc[0] | (vsc[1] << 8)), vs1 = scales_to_half(vsc[2] | (vsc[3] << 8));
@@ -364,7 +420,7 @@ __global__ void __launch_bounds__(THREADS) kv4_attn_warp_kernel(const __grid_con
             acc.x += f * x.x; acc.y += f * x.y; acc.z += f * x.z; acc.w += f * x.w;
         }
         const size_t row = q_row(vr);
-        if (a.split > 1) {
+        if (a.part_n) {
             const size_t p = (size_t)part * a.rows_total + row;
             *reinterpret_cast<float4*>(a.part_o + p * DH + c) = acc;
             if (c == 0) a.part_ml[p] = make_float2(mm, ll);
@@ -378,55 +434,63 @@ __global__ void __launch_bounds__(THREADS) kv4_attn_warp_kernel(const __grid_con
     }
 }
 
-// The parts of the rows put together in their order; a warp per row.
+// The parts of the rows put together, a CTA per row: its warps take eight parts at a time in turn, their sums are added in the warps' order.
 template <typename T, int DH>
 __global__ void __launch_bounds__(JOIN_THREADS) kv4_attn_join_kernel(const __grid_constant__ Args a) {
     KERNEL_PROLOGUE(24);   // kv4_attn_join_kernel
-    constexpr int PER = DH / 32;
-    const int lane = threadIdx.x & 31;
-    const long long row = (long long)blockIdx.x * (JOIN_THREADS / 32) + (threadIdx.x >> 5);
-    if (row >= a.rows_total) return;
-    const int parts = a.part_n ? __ldcg(a.part_n + row / ((long long)a.R * a.n_heads)) : a.split;
-    float2 ml[MAX_SPLIT / 32];
-    float mm = -INFINITY;
+    constexpr int PER = DH / 32, JW = JOIN_THREADS / 32;
+    __shared__ float wgt[MAX_SPLIT], sum[JW][DH];
+    __shared__ float red[2][JW];
+    const int t = threadIdx.x, lane = t & 31, warp = t >> 5;
+    const size_t row = blockIdx.x;
+    const int parts = __ldcg(a.part_n + row / ((size_t)a.R * a.n_heads));
+    float2 ml = make_float2(-INFINITY, 0.f);
+    static_assert(MAX_SPLIT <= JOIN_THREADS, "a part per thread");
+    if (t < parts) ml = __ldcg(a.part_ml + (size_t)t * a.rows_total + row);
+    const float wm = warp_max(ml.x);
+    if (lane == 0) red[0][warp] = wm;
+    __syncthreads();
+    float mm = red[0][0];
 #pragma unroll
-    for (int i = 0; i < MAX_SPLIT / 32; ++i) {
-        const int p = i * 32 + lane;
-        ml[i] = p < parts ? __ldcg(a.part_ml + (size_t)p * a.rows_total + row) : make_float2(-INFINITY, 0.f);
-        mm = fmaxf(mm, ml[i].x);
-    }
-    mm = warp_max(mm);
-    float ll = 0.f;
+    for (int i = 1; i < JW; ++i) mm = fmaxf(mm, red[0][i]);
+    const float f = ml.x == -INFINITY ? (ml.y == 0.f ? 0.f : 1.f) : ex2(ml.x - mm);        // (a part of NaN scores keeps its NaN)
+    if (t < MAX_SPLIT) wgt[t] = f;
+    const float ws = warp_sum(f * ml.y);
+    if (lane == 0) red[1][warp] = ws;
+    __syncthreads();
+    float ll = red[1][0];
 #pragma unroll
-    for (int i = 0; i < MAX_SPLIT / 32; ++i) {
-        ml[i].x = ml[i].x == -INFINITY ? (ml[i].y == 0.f ? 0.f : 1.f) : ex2(ml[i].x - mm);        // (a part of NaN scores keeps its NaN)
-        ll += ml[i].x * ml[i].y;
-    }
-    ll = warp_sum(ll);
+    for (int i = 1; i < JW; ++i) ll += red[1][i];
     float acc[PER];
 #pragma unroll
     for (int c = 0; c < PER; ++c) acc[c] = 0.f;
-    for (int p0 = 0; p0 < parts; p0 += 8) {    // eight parts' loads in flight
-        float f[8];
+    for (int p0 = 8 * warp; p0 < parts; p0 += 8 * JW) {
         float2 x[8][PER / 2];
+        float g[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const int p = p0 + i;                // (behind the last part: a weight of 0, as an empty part has, which has written no row)
-            f[i] = __shfl_sync(0xffffffffu, p < 32 ? ml[0].x : ml[MAX_SPLIT / 32 - 1].x, p & 31);
+            const int p = p0 + i;
+            g[i] = p < parts ? wgt[p] : 0.f;
             const float* src = a.part_o + ((size_t)p * a.rows_total + row) * DH + lane * PER;
 #pragma unroll
-            for (int c = 0; c < PER / 2; ++c) x[i][c] = f[i] != 0.f ? __ldcg(reinterpret_cast<const float2*>(src) + c) : make_float2(0.f, 0.f);
+            for (int c = 0; c < PER / 2; ++c) x[i][c] = p < parts ? __ldcg(reinterpret_cast<const float2*>(src) + c) : make_float2(0.f, 0.f);
         }
 #pragma unroll
         for (int i = 0; i < 8; ++i)
 #pragma unroll
-            for (int c = 0; c < PER / 2; ++c) { acc[2 * c] += f[i] * x[i][c].x; acc[2 * c + 1] += f[i] * x[i][c].y; }
+            for (int c = 0; c < PER / 2; ++c) { acc[2 * c] += g[i] * x[i][c].x; acc[2 * c + 1] += g[i] * x[i][c].y; }
     }
-    const float tv = a.tv ? __ldg(a.tv) : 1.f, inv = ll == 0.f ? 0.f : tv / ll;
-    T* out = (T*)a.out + (size_t)row * DH + lane * PER;
 #pragma unroll
-    for (int c = 0; c < PER; c += 2) store_pair<T>(out + c, acc[c] * inv, acc[c + 1] * inv);
-    if (lane == 0 && a.lse) a.lse[row] = ll == 0.f ? -INFINITY : (mm - LIFT + log2f(ll)) * 0.6931471805599453f;
+    for (int c = 0; c < PER; ++c) sum[warp][lane * PER + c] = acc[c];
+    __syncthreads();
+    const float tv = a.tv ? __ldg(a.tv) : 1.f, inv = ll == 0.f ? 0.f : tv / ll;
+    if (t < DH) {
+        float o = sum[0][t];
+#pragma unroll
+        for (int i = 1; i < JW; ++i) o += sum[i][t];
+        ((T*)a.out)[row * DH + t] = from_f<T>(o * inv);
+    }
+    if (t == 0 && a.lse) a.lse[row] = ll == 0.f ? -INFINITY : (mm - LIFT + log2f(ll)) * 0.6931471805599453f;
 }
 
 }  // namespace kv4

@@ -34,47 +34,11 @@ static_assert(TC_MMA_REGS + 2 * TC_SOFTMAX_REGS + TC_CODE_REGS <= 4 * TC_LAUNCH_
 constexpr size_t TC_SMEM = 1024 + (2 + TC_SLOTS) * (size_t)TC_TILE + 4 * TC_DEPTH * RAW_BYTES;
 static_assert(TC_SMEM <= 227 * 1024, "shared memory");
 
-constexpr int TC_MAX_BATCH = 32;                 // sequences whose parts are cut to measure (a lane each)
 struct TcArgs {
     Args a;
-    int batch;
     int tiles;                                   // CTAs per K/V head and part: row tiles (key split) or pairs of them
     int key_split;
-    int slots;                                   // parts per row tile and K/V head: batch <= TC_MAX_BATCH: at most, of equal length; else a.split for each sequence
 };
-
-// The part that slot number `slot` works on: sequence b, its part p of cnt, key tiles [t0, t0 + n).  False: more slots than parts.
-__device__ __forceinline__ bool find_part(const TcArgs& f, int slot, int& b, int& p, int& cnt, int& t0, int& n, int& len) {
-    const int lane = threadIdx.x & 31;
-    if (f.batch > TC_MAX_BATCH) {
-        b = slot / f.a.split; p = slot - b * f.a.split; cnt = f.a.split;
-        len = seq_len(f.a, b);
-        const int all = (len + TC_KEYS - 1) / TC_KEYS;
-        t0 = (int)((long long)all * p / cnt);
-        n = (int)((long long)all * (p + 1) / cnt) - t0;
-        return true;
-    }
-    const int my_len = lane < f.batch ? seq_len(f.a, lane) : 0, my = (my_len + TC_KEYS - 1) / TC_KEYS;
-    auto parts = [&](int size) { return lane < f.batch ? max(1, (my + size - 1) / size) : 0; };
-    int lo = 1, hi = max(1, __reduce_max_sync(0xffffffffu, my));          // (hi: a part for each sequence, which fits)
-    while (lo < hi) {
-        const int mid = (lo + hi) >> 1;
-        if (__reduce_add_sync(0xffffffffu, parts(mid)) <= f.slots) hi = mid; else lo = mid + 1;
-    }
-    const int mine = parts(lo);
-    int end = mine;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) { const int x = __shfl_up_sync(0xffffffffu, end, o); if (lane >= o) end += x; }
-    const unsigned hit = __ballot_sync(0xffffffffu, slot >= end - mine && slot < end);
-    if (hit == 0) return false;
-    b = __ffs(hit) - 1;
-    p = slot - __shfl_sync(0xffffffffu, end - mine, b);
-    cnt = __shfl_sync(0xffffffffu, mine, b);
-    len = __shfl_sync(0xffffffffu, my_len, b);
-    t0 = p * lo;
-    n = min(lo, __shfl_sync(0xffffffffu, my, b) - t0);
-    return true;
-}
 
 // ---- codes -> operand tiles ---------------------------------------------------------------------------------------------
 // A part's tiles in the order the tensor core takes them, two units (K and V) per key tile: K_0, V_0, K_1, V_1, ..., or, two key tiles in flight, K_0,
@@ -148,7 +112,7 @@ __device__ __forceinline__ void turn_codes(const Args& a, const Units& un, int b
             const int row = 8 * it + r8;
             asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w[it][0]), "=r"(w[it][1]), "=r"(w[it][2]), "=r"(w[it][3])
                          : "r"(raw + (uint32_t)(row * 64 + ((piece ^ ((row >> 1) & 3)) << 4))) : "memory");
-            asm volatile("{\n .reg .u16 h;\n ld.shared.u16 h, [%1];\n cvt.u32.u16 %0, h;\n}\n" : "=r"(sc[it]) : "r"(raw + CODE_BYTES + (uint32_t)(row * 8 + piece * 2)) : "memory");
+            asm volatile("ld.shared.u16 %0, [%1];" : "=r"(sc[it]) : "r"(raw + CODE_BYTES + (uint32_t)(row * 8 + piece * 2)) : "memory");
         }
 #pragma unroll
         for (int it = 0; it < 4; ++it) {
@@ -182,7 +146,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) kv4_attn_tc_kernel(const __grid
     __shared__ int abort_sh;
     const Args& a = f.a;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int tile = (int)blockIdx.x / f.slots, slot_no = (int)blockIdx.x - tile * f.slots, kvh = blockIdx.y;
+    const int tile = (int)blockIdx.x / a.slots, slot_no = (int)blockIdx.x - tile * a.slots, kvh = blockIdx.y;
     const int hpg = a.n_heads / a.n_kv;
     const long long vrows = (long long)hpg * a.R;
     const bool ksplit = f.key_split != 0;
@@ -216,9 +180,8 @@ __global__ void __launch_bounds__(TC_THREADS, 1) kv4_attn_tc_kernel(const __grid
     pdl_wait();            // lengths, codes and q may all come from the kernel before
     const uint32_t tmem_base = tmem_base_sh;
 
-    int b = 0, part = 0, parts = 0, t0 = 0, n = 0, len = 0;
-    const bool busy = find_part(f, slot_no, b, part, parts, t0, n, len);
-    if (busy && a.part_n && part == 0 && tile == 0 && kvh == 0 && threadIdx.x == 0) a.part_n[b] = parts;
+    int b = 0, part = 0, t0 = 0, n = 0, len = 0;
+    const bool busy = find_part<TC_KEYS>(a, slot_no, tile == 0 && kvh == 0 && threadIdx.x == 0, b, part, t0, n, len);
     const int cnt0 = ksplit ? (n + 1) >> 1 : n;                    // of stream 0 ...
     const int cnt1 = ksplit ? n >> 1 : (vr0 + TC_ROWS < vrows ? n : 0);       // ... and of stream 1
 

@@ -251,26 +251,30 @@ extern "C" int polestar_k_kv4_append(const void* k, const void* v, const int32_t
 
 constexpr size_t KV4_PARTS_BYTES = 65536 * sizeof(int);       // front of the scratch: parts of every sequence
 // Plans of the attention kernels: functions of the sizes alone, so that a scratch of polestar_k_kv4_scratch_bytes() bytes suffices for every call of
-// these sizes.  The warp-level kernel: tiles of 8 or 16 rows, parts of a fixed number of keys (those behind a short sequence's end leave at once).
-struct Kv4Warp { int tiles, rows, part_keys, split; };
+// these sizes.  Parts of the keys: up to MAX_BATCH sequences share `slots` of them, so that ragged lengths leave no SM idle, more have the same number each.
+static int kv4_slots(long long batch, long long wanted) {
+    wanted = std::max(batch, std::min(wanted, batch * kv4::MAX_SPLIT));
+    return (int)(batch > kv4::MAX_BATCH ? wanted / batch * batch : wanted);
+}
+static int kv4_parts(int batch, int slots) {         // of one sequence, at most
+    return batch > kv4::MAX_BATCH ? slots / batch : std::min(kv4::MAX_SPLIT, slots - batch + 1);
+}
+// The warp-level kernel: tiles of 8 or 16 rows, four CTAs for every SM, no part of a full sequence shorter than 512 keys, and none at all up to 1024 (joining
+// takes what it gains).
+struct Kv4Warp { int tiles, rows, slots; };
 static Kv4Warp kv4_warp_plan(long long batch, long long R, int cap, int n_heads, int n_kv) {
     const long long vrows = R * (n_heads / n_kv);
     Kv4Warp p;
     p.rows = vrows <= 8 ? 8 : 16;
     p.tiles = (int)((vrows + p.rows - 1) / p.rows);
-    const int step = kv4::CHUNK * kv4::WARPS;
-    const long long base = std::max<long long>(1, batch * n_kv * p.tiles);
-    const long long want = std::max<long long>(1, std::min<long long>(kv4::MAX_SPLIT, 6 * 148 / base));
-    p.part_keys = std::max<int>(512, (int)((cap + want - 1) / want));
-    p.part_keys = (p.part_keys + step - 1) / step * step;
-    p.split = (cap + p.part_keys - 1) / p.part_keys;
+    p.slots = kv4_slots(batch, std::min(4 * 148LL / std::max<long long>(1, (long long)n_kv * p.tiles), cap <= 1024 ? batch : batch * ((cap + 511) / 512)));
     return p;
 }
 // The tensor-core kernel, one CTA per SM: row tiles of 128, one per CTA with its keys split between the streams, or two per CTA.  Two share the turning of
 // codes (a pair takes 2.5 us for 128 keys, one tile 2.1, one of up to 64 rows 1.4), one gives more CTAs where there are few.  Whichever needs less time, by those figures and
 // 8.5 us of start and end, with the keys cut into the number of parts that does (3 us more for joining them); a part of a sequence that fills the cache is
 // no shorter than four key tiles.
-struct Kv4Tc { int tiles, key_split, slots, split, parts; double us; };
+struct Kv4Tc { int tiles, key_split, slots; double us; };
 static Kv4Tc kv4_tc_plan(long long batch, long long R, int cap, int n_heads, int n_kv) {
     const long long vrows = R * (n_heads / n_kv), row_tiles = (vrows + kv4::TC_ROWS - 1) / kv4::TC_ROWS, key_tiles = (cap + kv4::TC_KEYS - 1) / kv4::TC_KEYS;
     Kv4Tc p;
@@ -280,17 +284,14 @@ static Kv4Tc kv4_tc_plan(long long batch, long long R, int cap, int n_heads, int
         const long long tiles = one ? row_tiles : (row_tiles + 1) / 2, per = (long long)n_kv * tiles;
         const double tile_us = !one ? 2.5 : vrows <= 64 ? 1.4 : 2.1;
         for (int w = 0; w <= 8; ++w) {           // waves of CTAs; 0: a part for each sequence, whatever that takes
-            const long long s = w ? std::min(std::min(148LL * w / per, batch * key_tiles / 4), batch - 1 + kv4::MAX_SPLIT) : batch, c = s / batch;
+            const int slots = w ? kv4_slots(batch, std::min(148LL * w / per, batch * key_tiles / 4)) : (int)batch;
+            const long long c = slots / batch;
             if (w && c < 2) continue;
             const double us = (w ? (double)w : (double)((per * batch + 147) / 148)) * (double)((key_tiles + c - 1) / c) * tile_us + 8.5 + (w ? 3.0 : 0.0);
             if (us >= 0.97 * p.us) continue;
-            p.us = us; p.key_split = one; p.tiles = (int)tiles; p.slots = (int)s;
+            p.us = us; p.key_split = one; p.tiles = (int)tiles; p.slots = slots;
         }
     }
-    const bool same = batch > kv4::TC_MAX_BATCH;                           // the same number of parts for every sequence
-    if (same) p.slots = (int)(batch * (p.slots / batch));
-    p.split = same ? (int)(p.slots / batch) : 1;
-    p.parts = same ? p.split : (int)(p.slots - batch + 1);                 // at most, of one sequence
     return p;
 }
 // Which kernel: the warp-level one turns codes again for every 16 rows, the tensor-core one once for 128 or 256, but it starts slowly and its rows fill whole
@@ -303,11 +304,11 @@ static bool kv4_use_tc(int dtype, int head_dim, const Kv4Warp& w, const Kv4Tc& t
     if (dtype != POLESTAR_BF16 || head_dim != kv4::TC_DH) return false;
     const int forced = switch_kv4();
     if (forced) return forced == 2;
-    const double ctas = (double)batch * n_kv * w.tiles * w.split, part = (double)((std::min(cap, w.part_keys) + 127) / 128);
+    const double ctas = (double)w.slots * n_kv * w.tiles, part = std::ceil((double)((cap + 127) / 128) * batch / w.slots);
     const double all = (double)batch * n_kv * w.tiles * ((cap + 127) / 128);
     double tile = 1.4 + 1.8 * std::min(1.0, std::max(0.0, (ctas - 74) / 100));
     if (part >= 8) tile = std::min(tile, 2.4);
-    return t.us < std::max(all / 148 * 0.75, std::max(1.0, ctas / 444) * part * tile) + 5 + (w.split > 1 ? 3 : 0);
+    return t.us < std::max(all / 148 * 0.75, std::max(1.0, ctas / 444) * part * tile) + 5 + (w.slots > batch ? 3 : 0);
 }
 static bool kv4_attention_shape_ok(int batch, int R, int cap, int n_heads, int n_kv, int head_dim) {
     return kv4_shape_ok(batch, R, cap, n_kv, head_dim) && R <= 65536 && n_heads > 0 && n_heads <= 1024 && n_heads % n_kv == 0;
@@ -317,30 +318,32 @@ extern "C" size_t polestar_k_kv4_scratch_bytes(int32_t batch, int32_t R, int32_t
     if (!kv4_attention_shape_ok(batch, R, cap, n_heads, n_kv, head_dim)) return 0;
     const size_t rows = (size_t)batch * R * n_heads;
     if (rows == 0) return 256;
-    const int split = std::max(kv4_warp_plan(batch, R, cap, n_heads, n_kv).split, kv4_tc_plan(batch, R, cap, n_heads, n_kv).parts);
-    return 256 + KV4_PARTS_BYTES + (split > 1 ? split * rows * ((size_t)head_dim * 4 + 8) : 0);
+    const int parts = std::max(kv4_parts(batch, kv4_warp_plan(batch, R, cap, n_heads, n_kv).slots), kv4_parts(batch, kv4_tc_plan(batch, R, cap, n_heads, n_kv).slots));
+    return 256 + KV4_PARTS_BYTES + (parts > 1 ? parts * rows * ((size_t)head_dim * 4 + 8) : 0);
 }
 
-static dim3 join_grid(const kv4::Args& a) { return dim3((unsigned)((a.rows_total * 32 + kv4::JOIN_THREADS - 1) / kv4::JOIN_THREADS)); }
-static int launch_kv4_tc(const kv4::Args& a, const Kv4Tc& p, int batch, cudaStream_t st) {
+template <typename T, int DH>
+static int launch_kv4_join(const kv4::Args& a, cudaStream_t st) {
+    if (a.part_n) CK(launch_k(kv4::kv4_attn_join_kernel<T, DH>, dim3((unsigned)a.rows_total), dim3(kv4::JOIN_THREADS), 0, st, a));
+    return POLESTAR_OK;
+}
+static int launch_kv4_tc(const kv4::Args& a, const Kv4Tc& p, cudaStream_t st) {
     kv4::TcArgs f;
-    f.a = a; f.batch = batch; f.tiles = p.tiles; f.key_split = p.key_split; f.slots = p.slots;
+    f.a = a; f.tiles = p.tiles; f.key_split = p.key_split;
     if ((long long)p.tiles * p.slots > INT32_MAX) return POLESTAR_E_INVAL;
     CK(launch_k(kv4::kv4_attn_tc_kernel, dim3((unsigned)(p.tiles * p.slots), a.n_kv), dim3(kv4::TC_THREADS), kv4::TC_SMEM, st, f));
-    if (p.parts > 1) CK(launch_k(kv4::kv4_attn_join_kernel<__nv_bfloat16, 128>, join_grid(a), dim3(kv4::JOIN_THREADS), 0, st, a));
-    return POLESTAR_OK;
+    return launch_kv4_join<__nv_bfloat16, 128>(a, st);
 }
 template <typename T, int DH, int NB>
-static int launch_kv4_warp(const kv4::Args& a, const Kv4Warp& p, int batch, cudaStream_t st) {
-    if ((long long)p.tiles * p.split > INT32_MAX) return POLESTAR_E_INVAL;
-    CK(launch_k(kv4::kv4_attn_warp_kernel<T, DH, NB>, dim3((unsigned)(p.tiles * p.split), a.n_kv, batch), dim3(kv4::THREADS), kv4::warp_smem_bytes<DH, NB>(), st, a));
-    if (a.split > 1) CK(launch_k(kv4::kv4_attn_join_kernel<T, DH>, join_grid(a), dim3(kv4::JOIN_THREADS), 0, st, a));
-    return POLESTAR_OK;
+static int launch_kv4_warp(const kv4::Args& a, const Kv4Warp& p, cudaStream_t st) {
+    if ((long long)p.tiles * p.slots > INT32_MAX) return POLESTAR_E_INVAL;
+    CK(launch_k(kv4::kv4_attn_warp_kernel<T, DH, NB>, dim3((unsigned)(p.tiles * p.slots), a.n_kv), dim3(kv4::THREADS), kv4::warp_smem_bytes<DH, NB>(), st, a));
+    return launch_kv4_join<T, DH>(a, st);
 }
 template <typename T>
-static int launch_kv4_warp(const kv4::Args& a, const Kv4Warp& p, int head_dim, int batch, cudaStream_t st) {
-    if (head_dim == 128) return p.rows == 8 ? launch_kv4_warp<T, 128, 1>(a, p, batch, st) : launch_kv4_warp<T, 128, 2>(a, p, batch, st);
-    return p.rows == 8 ? launch_kv4_warp<T, 64, 1>(a, p, batch, st) : launch_kv4_warp<T, 64, 2>(a, p, batch, st);
+static int launch_kv4_warp(const kv4::Args& a, const Kv4Warp& p, int head_dim, cudaStream_t st) {
+    if (head_dim == 128) return p.rows == 8 ? launch_kv4_warp<T, 128, 1>(a, p, st) : launch_kv4_warp<T, 128, 2>(a, p, st);
+    return p.rows == 8 ? launch_kv4_warp<T, 64, 1>(a, p, st) : launch_kv4_warp<T, 64, 2>(a, p, st);
 }
 
 extern "C" int polestar_k_kv4_attention(const void* q, const uint8_t* kc, const uint8_t* ks, const uint8_t* vc, const uint8_t* vs,
@@ -359,20 +362,20 @@ extern "C" int polestar_k_kv4_attention(const void* q, const uint8_t* kc, const 
     if (rc) return rc;
     kv4::Args a;
     a.q = q; a.out = out; a.lse = lse; a.kc = kc; a.ks = ks; a.vc = vc; a.vs = vs; a.tk = k_scale; a.tv = v_scale; a.lens = lens;
-    a.R = R; a.cap = cap; a.n_heads = n_heads; a.n_kv = n_kv; a.rows_total = (long long)batch * R * n_heads;
+    a.batch = batch; a.R = R; a.cap = cap; a.n_heads = n_heads; a.n_kv = n_kv; a.rows_total = (long long)batch * R * n_heads;
     const Kv4Tc plan = kv4_tc_plan(batch, R, cap, n_heads, n_kv);
     const Kv4Warp wplan = kv4_warp_plan(batch, R, cap, n_heads, n_kv);
     const bool tc = kv4_use_tc(dtype, head_dim, wplan, plan, batch, cap, n_kv);
-    a.split = tc ? plan.split : wplan.split;
-    a.part_keys = wplan.part_keys;
-    a.part_n = tc && plan.parts > 1 ? (int*)scratch : nullptr;
+    a.slots = tc ? plan.slots : wplan.slots;
+    const int parts = kv4_parts(batch, a.slots);
+    a.part_n = parts > 1 ? (int*)scratch : nullptr;
     a.part_o = (float*)((char*)scratch + KV4_PARTS_BYTES);
-    a.part_ml = (float2*)((char*)a.part_o + (size_t)(tc ? plan.parts : wplan.split) * a.rows_total * head_dim * 4);
+    a.part_ml = (float2*)((char*)a.part_o + (size_t)parts * a.rows_total * head_dim * 4);
     a.scale = 1.0f / sqrtf((float)head_dim);
     cudaStream_t st = (cudaStream_t)stream;
-    if (tc) return launch_kv4_tc(a, plan, batch, st);
-    if (dtype == POLESTAR_BF16) return launch_kv4_warp<__nv_bfloat16>(a, wplan, head_dim, batch, st);
-    return launch_kv4_warp<float>(a, wplan, head_dim, batch, st);
+    if (tc) return launch_kv4_tc(a, plan, st);
+    if (dtype == POLESTAR_BF16) return launch_kv4_warp<__nv_bfloat16>(a, wplan, head_dim, st);
+    return launch_kv4_warp<float>(a, wplan, head_dim, st);
 }
 
 // ------------------------------------------------------------------------------------------
