@@ -38,7 +38,7 @@ struct Args {
     int batch, R, cap, n_heads, n_kv;
     int slots;                                   // parts per row tile and K/V head: up to MAX_BATCH sequences: at most, all of one length; beyond: the same number of each
     long long rows_total;                        // batch * R * n_heads
-    float scale;
+    double scale;                                // log2(e) / sqrt(head_dim)
 };
 
 __device__ __forceinline__ float ex2(float x) { float y; asm("ex2.approx.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
@@ -227,7 +227,7 @@ __global__ void __launch_bounds__(THREADS) kv4_attn_warp_kernel(const __grid_con
         top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
         const int e = min(max((int)(top >> 23), 1), 253);          // biased exponent of the largest magnitude
         const float down = __uint_as_float((uint32_t)(254 - e) << 23), up = __uint_as_float((uint32_t)e << 23);
-        const float un = up * (a.scale * 1.4426950408889634f * tk);
+        const float un = (float)((double)up * (a.scale * (double)tk));
         unit[n][0] = __shfl_sync(0xffffffffu, un, 8 * t);
         unit[n][1] = __shfl_sync(0xffffffffu, un, 8 * t + 4);
 #pragma unroll
@@ -249,7 +249,7 @@ __global__ void __launch_bounds__(THREADS) kv4_attn_warp_kernel(const __grid_con
     for (int i = 0; i < MT; ++i)
 #pragma unroll
         for (int n = 0; n < NB; ++n) o[i][n][0] = o[i][n][1] = o[i][n][2] = o[i][n][3] = 0.f;
-    float m[NB][2], most[NB][2], low[NB][2], l[NB][2];       // most = m + SLACK, low = m - LIFT (0 while m is -inf: p = 0 all the same), l: this lane's keys only
+    float m[NB][2], most[NB][2], low[NB][2], l[NB][2];       // most: LIFT + SLACK, low: m - LIFT (-inf and 0 while there is no m), l: this lane's keys only
 #pragma unroll
     for (int n = 0; n < NB; ++n)
 #pragma unroll
@@ -301,37 +301,38 @@ __global__ void __launch_bounds__(THREADS) kv4_attn_warp_kernel(const __grid_con
             }
         }
         bool grow = false;
-        float top[NB][2];
+        float y[NB][4];                          // score - m + LIFT
+        if (__builtin_expect(j0 + CHUNK > hi, 0)) {
 #pragma unroll
-        for (int n = 0; n < NB; ++n) {
-#pragma unroll
-            for (int x = 0; x < 4; ++x) s[n][x] *= unit[n][x & 1];
-            if (__builtin_expect(j0 + CHUNK > hi, 0)) {
+            for (int n = 0; n < NB; ++n) {
                 if (j0 + g >= hi) s[n][0] = s[n][1] = -INFINITY;
                 if (j0 + g + 8 >= hi) s[n][2] = s[n][3] = -INFINITY;
             }
+        }
+        auto relative = [&](int n, int x) { return s[n][x] == -INFINITY ? -INFINITY : fmaf(s[n][x], unit[n][x & 1], -low[n][x & 1]); };
 #pragma unroll
-            for (int x = 0; x < 2; ++x) {
-                top[n][x] = fmaxf(s[n][x], s[n][x + 2]);
-                grow |= top[n][x] > most[n][x];
-            }
+        for (int n = 0; n < NB; ++n) {
+#pragma unroll
+            for (int x = 0; x < 4; ++x) y[n][x] = relative(n, x);
+            grow |= fmaxf(y[n][0], y[n][2]) > most[n][0] || fmaxf(y[n][1], y[n][3]) > most[n][1];
         }
         if (__any_sync(0xffffffffu, grow)) {
 #pragma unroll
             for (int n = 0; n < NB; ++n)
 #pragma unroll
                 for (int x = 0; x < 2; ++x) {
-                    float nm = top[n][x];
+                    float nm = fmaxf(s[n][x], s[n][x + 2]);
 #pragma unroll
                     for (int d = 4; d < 32; d <<= 1) nm = fmaxf(nm, __shfl_xor_sync(0xffffffffu, nm, d));
-                    nm = nm > most[n][x] ? nm : m[n][x];
+                    nm = nm == -INFINITY ? nm : nm * unit[n][x];           // (unit >= 0: the maximum commutes with it)
+                    nm = nm > m[n][x] + SLACK ? nm : m[n][x];
                     const float f = m[n][x] == -INFINITY ? 0.f : ex2(m[n][x] - nm);
                     m[n][x] = nm;
-                    most[n][x] = nm + SLACK;
-                    low[n][x] = nm == -INFINITY ? 0.f : nm - LIFT;
+                    if (nm > -INFINITY) { most[n][x] = LIFT + SLACK; low[n][x] = nm - LIFT; }
                     l[n][x] *= f;
 #pragma unroll
                     for (int i = 0; i < MT; ++i) { o[i][n][x] *= f; o[i][n][x + 2] *= f; }
+                    y[n][x] = relative(n, x); y[n][x + 2] = relative(n, x + 2);
                 }
         }
         uint32_t pf[TERMS][NB][2];
@@ -339,7 +340,7 @@ __global__ void __launch_bounds__(THREADS) kv4_attn_warp_kernel(const __grid_con
         for (int n = 0; n < NB; ++n) {
             float p[4];
 #pragma unroll
-            for (int x = 0; x < 4; ++x) p[x] = ex2(s[n][x] - low[n][x & 1]);
+            for (int x = 0; x < 4; ++x) p[x] = ex2(y[n][x]);
             l[n][0] += p[0] + p[2];
             l[n][1] += p[1] + p[3];
 #pragma unroll

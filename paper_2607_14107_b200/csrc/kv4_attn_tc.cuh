@@ -306,7 +306,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) kv4_attn_tc_kernel(const __grid
         __syncwarp();
         if (lane == 0) mbar_arrive(bar_q);
         asm volatile("bar.sync 1, 256;" ::: "memory");             // the rows' units
-        const float unit = unit_sh[ksplit ? 0 : g][row] * (a.scale * 1.4426950408889634f * (a.tk ? __ldg(a.tk) : 1.f));
+        const float unit = (float)((double)unit_sh[ksplit ? 0 : g][row] * (a.scale * (double)(a.tk ? __ldg(a.tk) : 1.f)));
         const float tv = a.tv ? __ldg(a.tv) : 1.f;
 
         float m = -INFINITY, l = 0.f;

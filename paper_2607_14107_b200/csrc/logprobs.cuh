@@ -1,10 +1,11 @@
 // Log-probability of a given token, entropy and the most likely alternatives of logits rows, in one launch that reads every logit once from
 // global memory (a few of them twice, from L2).
 //
-//   m = max x,  S = sum e^(x - m),  Q = sum e^(x - m) (x - m)
-//   log p(v) = (x_v - m) - log S,   entropy = log S - Q / S       (relative to m, so that a nearly certain row keeps its small values)
+//   m = max x,  S = C + s = (entries equal to m) + sum of e^(x - m) over the others,  Q = sum e^(x - m) (x - m)
+//   log p(v) = (x_v - m) - log S,   entropy = log S - Q / S
+// Relative to m and with the entries that are m counted apart, a nearly certain row keeps its small values: log S = log C + log1p(s / C).
 //
-// A thread-block cluster of up to eight CTAs per row, as in the confidence kernel; every thread carries (m, S, Q) in 32 bits and
+// A thread-block cluster of up to eight CTAs per row, as in the confidence kernel; every thread carries (m, C, s, Q) in 32 bits and
 // rescales once per batch of loads.  Alternatives: the k-th largest of the maxima of 64 groups of threads is a lower bound of the k-th largest
 // logit, so only the pieces of threads whose own maximum reaches it are read again, dealt out over the whole CTA; what reaches the bound goes through a
 // buffer in shared memory as (value, index) keys, whose order is total: larger values first, lower indices first among equals.  If the buffer overflows (many equal
@@ -19,7 +20,8 @@ using namespace tc;
 
 constexpr int MAX_CL = 8, MAX_THREADS = 512, MAX_K = 32, SEGMENTS = 64, CAP = 1024, U = 4;
 
-// Sixteen bytes of logits: unpacked as they are, unpacked with -inf as the lowest finite value (NaN stays), and their largest (NaN left out).
+// Sixteen bytes of logits: unpacked as they are, unpacked with -inf as the lowest finite value (NaN stays), their largest (NaN left out), and the number of those
+// that are m, which -inf takes the place of.
 template <typename T> struct In;
 template <> struct In<float> {
     static constexpr int N = 4;
@@ -32,6 +34,11 @@ template <> struct In<float> {
 #pragma unroll
         for (int i = 0; i < 4; ++i) asm("max.NaN.f32 %0, %0, %1;" : "+f"(v[i]) : "f"(-3.4028234663852886e38f));
     }
+    static __device__ __forceinline__ int drop1(uint32_t& x, uint32_t m) { const bool hit = x == m; x = hit ? 0xff800000u : x; return hit; }
+    static __device__ __forceinline__ int drop(uint4& w, float m) {
+        const uint32_t b = __float_as_uint(m);
+        return drop1(w.x, b) + drop1(w.y, b) + drop1(w.z, b) + drop1(w.w, b);
+    }
     static __device__ __forceinline__ float top(const uint4& w) {
         return fmaxf(fmaxf(__uint_as_float(w.x), __uint_as_float(w.y)), fmaxf(__uint_as_float(w.z), __uint_as_float(w.w)));
     }
@@ -43,6 +50,16 @@ template <> struct In<__nv_bfloat16> {
     static __device__ __forceinline__ void unpack(const uint4& w, float* v) { spread(w.x, v); spread(w.y, v + 2); spread(w.z, v + 4); spread(w.w, v + 6); }
     static __device__ __forceinline__ uint32_t low(uint32_t x) { uint32_t y; asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(y) : "r"(x), "r"(0xff7fff7fu)); return y; }
     static __device__ __forceinline__ void finite(const uint4& w, float* v) { spread(low(w.x), v); spread(low(w.y), v + 2); spread(low(w.z), v + 4); spread(low(w.w), v + 6); }
+    static __device__ __forceinline__ int drop1(uint32_t& x, uint32_t m) {
+        const bool lo = (x << 16) == m, hi = (x & 0xffff0000u) == m;
+        x = lo ? (x & 0xffff0000u) | 0xff80u : x;
+        x = hi ? (x & 0xffffu) | 0xff800000u : x;
+        return (int)lo + (int)hi;
+    }
+    static __device__ __forceinline__ int drop(uint4& w, float m) {
+        const uint32_t b = __float_as_uint(m);
+        return drop1(w.x, b) + drop1(w.y, b) + drop1(w.z, b) + drop1(w.w, b);
+    }
     static __device__ __forceinline__ uint32_t max2(uint32_t x, uint32_t y) { uint32_t z; asm("max.bf16x2 %0, %1, %2;" : "=r"(z) : "r"(x), "r"(y)); return z; }
     static __device__ __forceinline__ float top(const uint4& w) {
         const uint32_t m = max2(max2(w.x, w.y), max2(w.z, w.w));
@@ -84,18 +101,29 @@ __device__ __forceinline__ float key_value(unsigned long long k) {
 __device__ __forceinline__ int key_index(unsigned long long k) { return (int)~(uint32_t)k; }
 
 __device__ __forceinline__ float ex2(float x) { float y; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
+__device__ __forceinline__ float redux_max(float v) {
+    float r;
+    asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(v));
+    return r;
+}
 constexpr float L2E = 1.4426950408889634f;
 
 struct Run {
-    float m = -INFINITY, s = 0.f, q = 0.f;
+    float m = -INFINITY, c = 0.f, s = 0.f, q = 0.f;
     // another part of the row
-    __device__ __forceinline__ void join(float om, float os, float oq) {
+    __device__ __forceinline__ void join(float om, float oc, float os, float oq) {
         const float nm = fmaxf(m, om), ref = nm == -INFINITY ? 0.f : nm;
         const float da = fmaxf(m - ref, -1e30f), db = fmaxf(om - ref, -1e30f);        // (an empty part: factor 0, no NaN from 0 * inf)
         const float fa = expf(da), fb = expf(db);
-        q = fa * (q + s * da) + fb * (oq + os * db);
-        s = fa * s + fb * os;
+        q = fa * (q + (c + s) * da) + fb * (oq + (oc + os) * db);
+        s = (m == nm ? s : fa * (c + s)) + (om == nm ? os : fb * (oc + os));
+        c = (m == nm ? c : 0.f) + (om == nm ? oc : 0.f);
         m = nm;
+    }
+    __device__ __forceinline__ void join_warp() {
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1)
+            join(__shfl_xor_sync(0xffffffffu, m, o), __shfl_xor_sync(0xffffffffu, c, o), __shfl_xor_sync(0xffffffffu, s, o), __shfl_xor_sync(0xffffffffu, q, o));
     }
 };
 
@@ -126,7 +154,7 @@ __global__ void __launch_bounds__(MAX_THREADS) token_logprobs_kernel(Args a) {
     Run r;
     float best = -INFINITY;                              // the largest alternative of this thread
     if (extra >= 0 && extra != a.mask_id) best = fmaxf(best, x_extra);
-    for (int i = c0 + t; i < c1; i += U * nt) {
+    for (int i = c0 + t; i - lane < c1; i += U * nt) {   // (a warp goes round together: it shares its running maximum)
         uint4 w[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) w[u] = i + u * nt < c1 ? __ldg(l4 + i + u * nt) : make_uint4(In<T>::PAD, In<T>::PAD, In<T>::PAD, In<T>::PAD);
@@ -147,13 +175,21 @@ __global__ void __launch_bounds__(MAX_THREADS) token_logprobs_kernel(Args a) {
             }
         }
         best = fmaxf(best, bb);
-        if (bm > r.m) {                                  // (rare after the first batches)
-            const float d = fmaxf(r.m - bm, -1e30f), f = ex2(d * L2E);
-            r.q = f * (r.q + r.s * d);
-            r.s *= f;
-            r.m = bm;
+        const float wm = redux_max(bm);
+        if (wm > r.m) {                                  // (rare after the first batches)
+            const float d = fmaxf(r.m - wm, -1e30f), f = ex2(d * L2E);
+            r.q = f * (r.q + (r.c + r.s) * d);
+            r.s = f * (r.c + r.s);
+            r.c = 0.f;
+            r.m = wm;
         }
         if (__builtin_expect(r.m >= -1e38f, 1)) {
+            if (wm == r.m) {                             // the entries that are the maximum are counted apart
+                int c = 0;
+#pragma unroll
+                for (int u = 0; u < U; ++u) c += In<T>::drop(w[u], r.m);
+                r.c += (float)c;
+            }
             // -inf as the lowest finite value: p = 0 all the same, and p z = 0
             const uint64_t nm2 = f2_pack(-r.m, -r.m), l2e = f2_pack(L2E, L2E);
             uint64_t s2[2] = {0ull, 0ull}, q2[2] = {0ull, 0ull};
@@ -173,7 +209,8 @@ __global__ void __launch_bounds__(MAX_THREADS) token_logprobs_kernel(Args a) {
             }
             r.s += f2_sum(f2_add(s2[0], s2[1]));
             r.q += f2_sum(f2_add(q2[0], q2[1]));
-        } else {                                         // (nothing above the lowest values so far: -inf is told from them)
+        } else {
+            // nothing above the lowest values has come so far: -inf is told from them
             const float ref = r.m == -INFINITY ? 0.f : r.m;
 #pragma unroll
             for (int u = 0; u < U; ++u) {
@@ -182,16 +219,16 @@ __global__ void __launch_bounds__(MAX_THREADS) token_logprobs_kernel(Args a) {
 #pragma unroll
                 for (int e = 0; e < N; ++e) {
                     const float z = fmaxf(v[e] - ref, -1e30f), p = v[e] == v[e] ? (v[e] == -INFINITY ? 0.f : ex2(z * L2E)) : v[e];
-                    r.s += p;
+                    const bool top = v[e] == r.m && r.m > -INFINITY;
+                    r.c += top ? 1.f : 0.f;
+                    r.s += top ? 0.f : p;
                     r.q += p * z;
                 }
             }
         }
     }
-    if (extra >= 0) r.join(x_extra, x_extra == x_extra ? (x_extra > -INFINITY ? 1.f : 0.f) : x_extra, 0.f);
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1)
-        r.join(__shfl_xor_sync(0xffffffffu, r.m, o), __shfl_xor_sync(0xffffffffu, r.s, o), __shfl_xor_sync(0xffffffffu, r.q, o));
+    if (extra >= 0) r.join(x_extra, x_extra > -INFINITY ? 1.f : 0.f, x_extra == x_extra ? 0.f : x_extra, 0.f);
+    r.join_warp();
 
     // ---- the CTA's k largest alternatives: candidates in buf[0 .. n) ----
     int n = 0;
@@ -257,7 +294,7 @@ __global__ void __launch_bounds__(MAX_THREADS) token_logprobs_kernel(Args a) {
     if (cl > 1) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
     if (lane == 0) {
         const uint32_t dst = dsmem_addr((uint32_t)__cvta_generic_to_shared(parts + ch * nw + wid), 0);
-        asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(dst), "f"(r.m), "f"(r.s), "f"(r.q), "f"(0.f) : "memory");
+        asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(dst), "f"(r.m), "f"(r.c), "f"(r.s), "f"(r.q) : "memory");
     }
     if (a.k > 0) {
         const uint32_t list = dsmem_addr((uint32_t)__cvta_generic_to_shared(tops + ch * a.k), 0);
@@ -273,20 +310,18 @@ __global__ void __launch_bounds__(MAX_THREADS) token_logprobs_kernel(Args a) {
     if (ch != 0) return;
     // every warp of the first CTA puts the parts together in the same fixed order
     Run f;
-    for (int c = lane; c < cl * nw; c += 32) f.join(parts[c].x, parts[c].y, parts[c].z);
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1)
-        f.join(__shfl_xor_sync(0xffffffffu, f.m, o), __shfl_xor_sync(0xffffffffu, f.s, o), __shfl_xor_sync(0xffffffffu, f.q, o));
+    for (int i = lane; i < cl * nw; i += 32) f.join(parts[i].x, parts[i].y, parts[i].z, parts[i].w);
+    f.join_warp();
     if (f.m > 1e30f) f.q = 0.f;          // floats there are 1e22 apart: p is 1 or 0, and Q exactly 0 (p z may have been 0 * inf)
-    const float ls = logf(f.s);
-    // (a row without an entry above -inf, or with an infinite one: S = 0; one with NaN: S is NaN.  All its results are NaN.)
+    // (a row without an entry above -inf: C = s = 0; one with NaN: s is NaN.  These rows' results, and those of one with +inf, are all NaN.)
+    const float sum = f.m < INFINITY ? f.c + f.s : __uint_as_float(0x7fc00000u), ls = f.c > 1.f ? logf(f.c) + log1pf(f.s / f.c) : log1pf(f.s);
     if (t == 0) {
-        if (a.entropy) a.entropy[row] = f.s > 0.f ? fmaxf(ls - f.q / f.s, 0.f) : __uint_as_float(0x7fc00000u);
+        if (a.entropy) a.entropy[row] = sum > 0.f ? fmaxf(ls - f.q / sum, 0.f) : __uint_as_float(0x7fc00000u);
         if (a.logprob) {
             const int v = a.target[row];
             float lp = 0.f;
             if (v >= a.V) lp = __uint_as_float(0x7fc00000u);
-            else if (v >= 0) lp = f.s > 0.f ? (to_f<T>(l[v]) - f.m) - ls : __uint_as_float(0x7fc00000u);
+            else if (v >= 0) lp = sum > 0.f ? (to_f<T>(l[v]) - f.m) - ls : __uint_as_float(0x7fc00000u);
             a.logprob[row] = lp;
         }
     }
@@ -301,7 +336,7 @@ __global__ void __launch_bounds__(MAX_THREADS) token_logprobs_kernel(Args a) {
         if (above >= a.k) continue;
         const size_t at = (size_t)row * a.k + above;
         a.top_ids[at] = k0 ? key_index(k0) : -1;         // fewer alternatives than asked for
-        a.top_logprobs[at] = k0 && f.s > 0.f ? (key_value(k0) - f.m) - ls : (k0 ? __uint_as_float(0x7fc00000u) : -INFINITY);
+        a.top_logprobs[at] = k0 && sum > 0.f ? (key_value(k0) - f.m) - ls : (k0 ? __uint_as_float(0x7fc00000u) : -INFINITY);
     }
 }
 

@@ -371,7 +371,7 @@ extern "C" int polestar_k_kv4_attention(const void* q, const uint8_t* kc, const 
     a.part_n = parts > 1 ? (int*)scratch : nullptr;
     a.part_o = (float*)((char*)scratch + KV4_PARTS_BYTES);
     a.part_ml = (float2*)((char*)a.part_o + (size_t)parts * a.rows_total * head_dim * 4);
-    a.scale = 1.0f / sqrtf((float)head_dim);
+    a.scale = 1.4426950408889634 / std::sqrt((double)head_dim);
     cudaStream_t st = (cudaStream_t)stream;
     if (tc) return launch_kv4_tc(a, plan, st);
     if (dtype == POLESTAR_BF16) return launch_kv4_warp<__nv_bfloat16>(a, wplan, head_dim, st);
