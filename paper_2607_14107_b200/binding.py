@@ -549,13 +549,19 @@ def polestar_k_fp4_scale_bytes(rows: int, d: int, fmt: int, layout: int) -> int:
     return int(load().polestar_k_fp4_scale_bytes(rows, d, fmt, layout))
 
 
+def _scale_bytes(rows: int, d: int, fmt: int, layout: int) -> int:
+    """The same for arguments that the call itself checks."""
+    groups = d // fp4_group(fmt)
+    return rows * groups if layout == SCALES_ROWS else (rows + 127) // 128 * ((groups + 3) // 4) * 512
+
+
 def polestar_k_fp4_quantize(x, codes, scales, fmt: int, layout: int = SCALES_ROWS, tensor_scale=None, deq=None):
     """x [rows][d] (rows may be strided) -> codes uint8 [rows][d/2], scales uint8 of polestar_k_fp4_scale_bytes() bytes, deq like x."""
     dev = _device("x", x)
     ld = _row_stride("x", x, dev)
     rows, d = x.shape
     lib = load()
-    if d % 32 or scales.numel() != lib.polestar_k_fp4_scale_bytes(rows, d, fmt, layout):
+    if d % 32 or scales.numel() != _scale_bytes(rows, d, fmt, layout):
         _refuse(f"scales have {scales.numel()} bytes, which is not what {rows} rows of {d} channels take")
     _check(lib.polestar_k_fp4_quantize(
         x.data_ptr(), ld, rows, d, _dtype_code(x), fmt, layout, _factor("tensor_scale", tensor_scale, dev),
@@ -570,7 +576,7 @@ def polestar_k_fp4_matmul(a_codes, a_scales, b_codes, b_scales, out, fmt: int, a
         _refuse("codes have to be matrices")
     (M, half), N = a_codes.shape, b_codes.shape[0]
     lib = load()
-    size = lib.polestar_k_fp4_scale_bytes
+    size = _scale_bytes
     if half % 32 or a_scales.numel() != size(M, 2 * half, fmt, SCALES_TILED) or b_scales.numel() != size(N, 2 * half, fmt, SCALES_TILED):
         _refuse(f"scales have {a_scales.numel()} and {b_scales.numel()} bytes, which is not what {M} and {N} rows of {2 * half} channels take")
     ld = _row_stride("out", out, dev)
