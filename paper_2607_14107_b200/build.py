@@ -4,6 +4,7 @@ from __future__ import annotations
 import os
 import subprocess
 import sys
+import time
 from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
@@ -55,6 +56,7 @@ def build(force: bool = False, verbose: bool = False, trace: bool = False) -> st
     nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
     arch = ["-gencode", "arch=compute_100a,code=sm_100a"]
     os.makedirs(OBJ, exist_ok=True)
+    started = time.time()                                  # outputs carry this time: a file edited during the build is newer than they are
 
     def compile_unit(name: str) -> str:
         stem = os.path.join(OBJ, name + ("_trace" if trace else ""))
@@ -66,13 +68,16 @@ def build(force: bool = False, verbose: bool = False, trace: bool = False) -> st
             cmd.insert(1, "-DPOLESTAR_TRACE")
         if verbose:
             cmd[1:1] = ["-Xptxas", "-v"]
-        return _run(cmd)
+        said = _run(cmd)
+        os.utime(stem + ".o", (started, started))
+        return said
 
     with ThreadPoolExecutor(len(UNITS)) as pool:
         said = list(pool.map(compile_unit, UNITS))
     if verbose:
         sys.stderr.write("".join(said))
     _run([nvcc, "-shared", *arch, *[os.path.join(OBJ, n + ("_trace" if trace else "") + ".o") for n in UNITS], "-o", out])
+    os.utime(out, (started, started))
     return out
 
 

@@ -226,7 +226,8 @@ __global__ void __launch_bounds__(THREADS) kv4_attn_warp_kernel(const __grid_con
         top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
         top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
         const int e = min(max((int)(top >> 23), 1), 253);          // biased exponent of the largest magnitude
-        const float down = __uint_as_float((uint32_t)(254 - e) << 23), up = __uint_as_float((uint32_t)e << 23);
+        // (infinity or NaN in q: every score of the row is NaN, not -inf, which is a key that is not there)
+        const float down = top >= 0x7f800000u ? __uint_as_float(0x7fc00000u) : __uint_as_float((uint32_t)(254 - e) << 23), up = __uint_as_float((uint32_t)e << 23);
         const float un = (float)((double)up * (a.scale * (double)tk));
         unit[n][0] = __shfl_sync(0xffffffffu, un, 8 * t);
         unit[n][1] = __shfl_sync(0xffffffffu, un, 8 * t + 4);

@@ -292,7 +292,8 @@ __global__ void __launch_bounds__(TC_THREADS, 1) kv4_attn_tc_kernel(const __grid
 #pragma unroll
                     for (int o = 1; o < 16; o <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
                     const int e = min(max((int)(top >> 23), 1), 253);
-                    const float down = __uint_as_float((uint32_t)(254 - e) << 23);
+                    // (infinity or NaN in q: every score of the row is NaN, not -inf)
+                    const float down = top >= 0x7f800000u ? __uint_as_float(0x7fc00000u) : __uint_as_float((uint32_t)(254 - e) << 23);
                     if (ch == 0) unit_sh[ksplit ? 0 : g][lr] = __uint_as_float((uint32_t)e << 23);
                     uint32_t h[4];
 #pragma unroll

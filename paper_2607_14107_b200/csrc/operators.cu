@@ -36,6 +36,7 @@ struct DevInfo { bool ready = false; int sm_count = 0; int gemm_pairs = 0; };   
 static const int MAX_DEVICES = 64;
 static std::mutex g_mu;
 static DevInfo g_dev[MAX_DEVICES];
+namespace ps { void note_sm_count(int n); }               // polestar.cu: what polestar_sm_count() answers
 static cudaError_t set_kernel_attributes();
 static int resident_gemm_pairs(int sms);
 static int device_info(DevInfo* out) {
@@ -50,6 +51,7 @@ static int device_info(DevInfo* out) {
         di.gemm_pairs = resident_gemm_pairs(di.sm_count);
         di.ready = true;
     }
+    note_sm_count(di.sm_count);
     *out = di;
     return POLESTAR_OK;
 }

@@ -107,7 +107,8 @@ struct AttnClusters { int n[atc::MAX_KT][atc::MAX_CL + 1] = {}; };
 struct DevInfo { bool ready = false; int sm_count = 0; int gemm_pairs = 0; AttnClusters attn; };
 static const int MAX_DEVICES = 64;
 static DevInfo g_dev[MAX_DEVICES];
-static int g_last_sm_count = 0;
+static std::atomic<int> g_last_sm_count{0};
+namespace ps { void note_sm_count(int n) { g_last_sm_count.store(n); } }      // (operators.cu)
 
 static cudaError_t set_kernel_attributes();
 static int resident_gemm_pairs();

@@ -1,6 +1,8 @@
 """Single-kernel timings through the C ABI: the refresh micro-benchmark (select -> gathered QKV
 refresh -> scatter, 4096 cache positions x 4096 hidden, refresh fraction 1..100 %, batch 1 and 8),
-the hidden-delta stream, the drift kernel at the 8B shapes and the confidence kernel.
+the hidden-delta stream, the drift kernel at the 8B shapes and the confidence kernel; and the
+operators next to the decoding path: 4-bit rows and their product, attention over a 4-bit K/V
+cache, token log-probabilities.
 
     python -m paper_2607_14107_b200.kernel_bench [--quick] [--only select,refresh,...]
 
@@ -164,13 +166,81 @@ def bench_confidence(quick):
         emit("confidence", us, rows * V * 4, 0, {"rows": rows, "vocab": V})
 
 
+def bench_fp4(quick):
+    # activations quantised, then multiplied by 4-bit weights: a decode step's rows and a block entry's, widths of the 8B shape.  TFLOP/s of
+    # the 4-bit products; their peak is nominally four times that of bf16.
+    for rows, n, k in ((32, 12288, 4096), (32, 4096, 12288), (128, 12288, 4096), (512, 12288, 4096), (4096, 12288, 4096), (16384, 4096, 4096)):
+        if quick and rows > 512:
+            continue
+        n_copy = max(2, min(12, int(4e8 / (n * k / 2))))
+        groups = k // 16
+        x = [I.normal_tensor(I.tensor_key(9, c, 1), (rows, k), 1.0, torch.bfloat16, "cuda") for c in range(2)]
+        t = torch.ones(1, device="cuda")
+        xc = torch.empty((rows, k // 2), dtype=torch.uint8, device="cuda")
+        xs = torch.empty(Bd.polestar_k_fp4_scale_bytes(rows, k, Bd.FP4_NV, Bd.SCALES_TILED), dtype=torch.uint8, device="cuda")
+        us = timed(lambda i: Bd.polestar_k_fp4_quantize(x[i % 2], xc, xs, Bd.FP4_NV, Bd.SCALES_TILED, tensor_scale=t), 30)
+        emit("fp4_quantize", us, rows * k * 2 + rows * k // 2 + rows * groups, 0, {"rows": rows, "d": k, "format": "nv"})
+        ws = []
+        for c in range(n_copy):
+            w = I.normal_tensor(I.tensor_key(9, c, 2), (n, k), 1.0, torch.bfloat16, "cuda")
+            wc = torch.empty((n, k // 2), dtype=torch.uint8, device="cuda")
+            wsc = torch.empty(Bd.polestar_k_fp4_scale_bytes(n, k, Bd.FP4_NV, Bd.SCALES_TILED), dtype=torch.uint8, device="cuda")
+            Bd.polestar_k_fp4_quantize(w, wc, wsc, Bd.FP4_NV, Bd.SCALES_TILED, tensor_scale=t)
+            ws.append((wc, wsc))
+            del w
+        out = torch.empty((rows, n), dtype=torch.bfloat16, device="cuda")
+        us = timed(lambda i: Bd.polestar_k_fp4_matmul(xc, xs, *ws[i % n_copy], out, Bd.FP4_NV, a_tensor_scale=t, b_tensor_scale=t), 30)
+        emit("fp4_matmul", us, (n + rows) * (k // 2 + groups) + rows * n * 2, 2.0 * rows * n * k, {"rows": rows, "n": n, "k": k, "format": "nv"})
+
+
+def bench_kv4(quick):
+    # one token of long ragged sequences; a decode step's rows of the 8B shape; a refresh of many rows; rows entering the cache
+    for name, bs, R, cap, nh, nkv in (("token", 8, 1, 32768, 28, 4), ("c2 window+block", 1, 128, 512, 32, 32), ("c2 block entry", 1, 512, 512, 32, 32),
+                                      ("c4 per sequence", 1, 192, 2048, 32, 32), ("refresh", 1, 128, 32768, 28, 4)):
+        if quick and not name.startswith("c2"):
+            continue
+        dh, t = 128, torch.full((1,), 0.05, device="cuda")
+        n_copy = max(2, min(24, int(4e8 / (bs * cap * nkv * dh))))
+        caches = []
+        rows = torch.arange(cap, dtype=torch.int32, device="cuda")[None].repeat(bs, 1)
+        for c in range(n_copy):
+            new = [I.normal_tensor(I.tensor_key(11, c, i), (bs, cap, nkv * dh), 1.0, torch.bfloat16, "cuda") for i in (1, 2)]
+            codes = [torch.empty((bs, cap, nkv, dh // 2), dtype=torch.uint8, device="cuda") for _ in range(2)]
+            scales = [torch.empty((bs, cap, nkv, dh // 16), dtype=torch.uint8, device="cuda") for _ in range(2)]
+            put = lambda: Bd.polestar_k_kv4_append(*new, rows, None, codes[0], scales[0], codes[1], scales[1], t, t)  # noqa: E731
+            put()
+            caches.append((codes[0], scales[0], codes[1], scales[1]))
+        us = timed(lambda i: put(), 20)
+        emit("kv4_append", us, bs * cap * nkv * dh * (4 + 1 + 1 / 8), 0, {"shape": name, "batch": bs, "rows": cap, "heads": [nh, nkv]})
+        q = I.normal_tensor(I.tensor_key(11, 0, 3), (bs, R, nh * dh), 1.0, torch.bfloat16, "cuda")
+        lens = torch.tensor([max(1, cap * (8 - i) // 8) for i in range(bs)], dtype=torch.int32, device="cuda")
+        out, lse = torch.empty_like(q), torch.empty((bs, R, nh), device="cuda")
+        scratch = torch.empty(Bd.polestar_k_kv4_scratch_bytes(bs, R, cap, nh, nkv, dh), dtype=torch.uint8, device="cuda")
+        us = timed(lambda i: Bd.polestar_k_kv4_attention(q, *caches[i % n_copy], t, t, lens, out, lse, scratch), 48)
+        keys = int(lens.sum())
+        emit("kv4_attention", us, keys * nkv * dh * (1 + 1 / 8) + 2 * q.numel() * 2, 4.0 * R * keys * nh * dh,
+             {"shape": name, "batch": bs, "rows": R, "keys": keys, "heads": [nh, nkv]})
+
+
+def bench_logprobs(quick):
+    V = 126464
+    for rows, dtype, top in ((32, torch.float32, 0), (32, torch.float32, 8), (512, torch.float32, 8), (512, torch.bfloat16, 20)):
+        n = 8 if rows == 32 else 2
+        lg = [I.normal_tensor(I.tensor_key(7, c, 1), (rows, V), 3.0, torch.float32, "cuda").to(dtype) for c in range(n)]
+        target = torch.arange(rows, dtype=torch.int32, device="cuda")
+        lp, h = torch.empty(rows, device="cuda"), torch.empty(rows, device="cuda")
+        ids, tops = torch.empty((rows, top), dtype=torch.int32, device="cuda"), torch.empty((rows, top), device="cuda")
+        us = timed(lambda i: Bd.polestar_k_token_logprobs(lg[i % n], target, V - 1, lp, h, ids, tops), 30)
+        emit("token_logprobs", us, rows * V * lg[0].element_size(), 0, {"rows": rows, "vocab": V, "dtype": str(dtype)[6:], "alternatives": top})
+
+
 def main():
     ap = argparse.ArgumentParser()
     ap.add_argument("--quick", action="store_true")
-    ap.add_argument("--only", default="select,refresh,hidden_delta,drift,confidence")
+    ap.add_argument("--only", default="select,refresh,hidden_delta,drift,confidence,fp4,kv4,logprobs")
     a = ap.parse_args()
     fns = {"select": bench_select, "refresh": bench_refresh, "hidden_delta": bench_hidden_delta, "drift": bench_drift,
-           "confidence": bench_confidence}
+           "confidence": bench_confidence, "fp4": bench_fp4, "kv4": bench_kv4, "logprobs": bench_logprobs}
     for name in a.only.split(","):
         fns[name](a.quick)
 

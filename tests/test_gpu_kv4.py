@@ -166,6 +166,31 @@ def test_nan_rows_stay_their_own():
     assert torch.equal(o[keep], clean.view(R, nh, dh)[keep])
 
 
+@pytest.mark.parametrize("kernel,dtype", [(1, "bf16"), (2, "bf16"), (0, "f32")])
+@pytest.mark.parametrize("cap", [1, 77, 3000])
+def test_infinite_q_is_nan_whatever_its_scores_sign(monkeypatch, kernel, dtype, cap):
+    # every score is -inf: softmax over them is NaN, and not the zero row of a sequence without keys
+    monkeypatch.setenv("POLESTAR_KV4_KERNEL", str(kernel))
+    Bd.polestar_reload_env()
+    R, dh, t = 3, 128, torch.tensor([0.02], device="cuda")
+    k = torch.ones((2, cap, dh), dtype=DT[dtype], device="cuda")
+    c = [torch.empty((2, cap, 1, n), dtype=torch.uint8, device="cuda") for n in (dh // 2, dh // 16, dh // 2, dh // 16)]
+    Bd.polestar_k_kv4_append(k, k, None, None, *c, t, t)
+    q = torch.ones((2, R, dh), dtype=DT[dtype], device="cuda")
+    q[:, 1, 5] = -math.inf
+    out, lse = run(q, *c, 0.02, 0.02, [cap, 0])
+    assert torch.isnan(out[0, 1]).all() and torch.isnan(lse[0, 1]).all()
+    assert not out[1].any() and torch.isinf(lse[1]).all()                  # (no keys: zeros)
+    assert torch.isfinite(out[0, ::2]).all() and torch.isfinite(lse[0, ::2]).all()
+
+
+@pytest.mark.parametrize("kernel,dtype", [(1, "bf16"), (2, "bf16"), (0, "f32")])
+def test_more_sequences_than_are_cut_to_measure(monkeypatch, kernel, dtype):
+    monkeypatch.setenv("POLESTAR_KV4_KERNEL", str(kernel))
+    Bd.polestar_reload_env()
+    check(dtype, 40, 1, 2200, 4, 2, 128, [2200, 0, 1, 64, 65] + [(97 * i) % 2201 for i in range(35)], seed=8)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_without_lse_and_without_lengths(dtype):
     out, lse, c, q = check(dtype, 2, 9, 400, 4, 4, 64, None)
