@@ -12,6 +12,7 @@
 // load and store of a warp is contiguous whatever the type; the lanes of a group find its maximum by shuffles.
 #pragma once
 #include <cuda_fp16.h>
+#include <climits>
 
 #include "tcgen05.cuh"
 
@@ -225,7 +226,7 @@ struct AppendArgs {
     const int* idx; const int* counts;           // [batch][R] positions, [batch] rows listed (null: R)
     int R, cap, width, rows_per_block;
 };
-constexpr int APPEND_MAX_ROWS = 64;              // rows of a block
+constexpr int APPEND_MAX_ROWS = 256;             // rows of a block
 
 // blockIdx: x = rows_per_block rows, y = sequence, z = K or V.  A row that lists a position outside the cache is skipped, and so is one whose
 // position a later row lists again: the last one listed stays, whole.
@@ -243,15 +244,42 @@ __global__ void __launch_bounds__(THREADS) kv_append_kernel(const __grid_constan
         // (stored values of rows that are not listed are left as they were)
         return;
     }
-    const int live = r1 - r0;
+    const int live = r1 - r0, ppr = a.width / N, total = live * ppr;
+    const uint4* x = reinterpret_cast<const uint4*>((const T*)a.x[which] + (seq * a.R + r0) * a.width);
+    constexpr int PER = 4;
+    uint4 w[PER];
+    auto load = [&](int b) {
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const int at = b + i * THREADS + threadIdx.x;
+            w[i] = at < total ? __ldg(x + at) : make_uint4(0u, 0u, 0u, 0u);
+        }
+    };
+    load(0);                                     // (under way while the list is looked through)
     for (int i = threadIdx.x; i < live; i += THREADS) {
         const int p = idx ? idx[r0 + i] : r0 + i;
         pos[i] = p >= 0 && p < a.cap ? p : -1;
     }
     // an ascending rest of the list, as a selection writes it, has nothing twice; any other is compared entry by entry
     bool ascending = true;
-    if (idx)
-        for (int j = r0 + 1 + threadIdx.x; j < count; j += THREADS) ascending = ascending && __ldg(idx + j) > __ldg(idx + j - 1);
+    if (idx) {
+        constexpr int AHEAD = 8;
+        const int lane = threadIdx.x & 31;
+        for (int j0 = r0 + (int)(threadIdx.x & ~31u); j0 < count; j0 += AHEAD * THREADS) {
+            int v[AHEAD], last[AHEAD];           // entry j, and the entry behind the warp's last one
+#pragma unroll
+            for (int i = 0; i < AHEAD; ++i) {
+                const int j = j0 + i * THREADS + lane;
+                v[i] = j < count ? __ldg(idx + j) : INT_MAX;
+                last[i] = lane == 31 && j + 1 < count ? __ldg(idx + j + 1) : INT_MAX;
+            }
+#pragma unroll
+            for (int i = 0; i < AHEAD; ++i) {
+                const int down = __shfl_down_sync(0xffffffffu, v[i], 1), next = lane == 31 ? last[i] : down;
+                ascending = ascending && (next > v[i] || next == INT_MAX);
+            }
+        }
+    }
     if (!__syncthreads_and(ascending)) {
         for (int j = r0 + 1 + threadIdx.x; j < count; j += THREADS) {
             const int p = __ldg(idx + j);
@@ -260,20 +288,12 @@ __global__ void __launch_bounds__(THREADS) kv_append_kernel(const __grid_constan
         }
         __syncthreads();
     }
-    const int ppr = a.width / N, total = live * ppr;
     const Factor t = make_factor<NV>(a.t[which]);
-    const uint4* x = reinterpret_cast<const uint4*>((const T*)a.x[which] + (seq * a.R + r0) * a.width);
     uint4* deq = a.deq[which] ? reinterpret_cast<uint4*>((T*)a.deq[which] + (seq * a.R + r0) * a.width) : nullptr;
     uint8_t* codes = a.codes[which] + seq * a.cap * (size_t)(a.width >> 1);
     uint8_t* scales = a.scales[which] + seq * a.cap * (size_t)(a.width >> 4);
-    constexpr int PER = 4;
     for (int b = 0; b < total; b += PER * THREADS) {
-        uint4 w[PER];
-#pragma unroll
-        for (int i = 0; i < PER; ++i) {
-            const int at = b + i * THREADS + threadIdx.x;
-            w[i] = at < total ? __ldg(x + at) : make_uint4(0u, 0u, 0u, 0u);
-        }
+        if (b > 0) load(b);
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
             if (b + i * THREADS >= total) break;     // (the same for all threads)

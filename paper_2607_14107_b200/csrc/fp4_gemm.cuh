@@ -57,32 +57,37 @@ struct GemmArgs {
     const float* ta; const float* tb;            // factors of the tensors (null: 1)
     void* out; long long ld;
     int M, N, K;
-    int split;                                   // CTAs of a cluster that share the K of a tile
+    int split, stages;                           // few rows: CTAs of a cluster that share the K of a tile, ring slots of a CTA
     int box_out;                                 // output rows, their stride and base are whole 16 bytes: they leave as tensor stores
 };
 
 // ---- few rows of A: bound by the stream of B ---------------------------------------------------------------------------
 // The wide matrix takes the 128 lanes: D^T = B A^T, a tile is 128 columns of the output x T rows of it, so a few rows cost no padding of the
-// stream.  The CTAs of a cluster (up to eight, while that leaves SMs to fill) take consecutive parts of K; each then hands its partial sums to
-// the CTA that owns the output rows (through distributed shared memory), which adds them in the order of K.
+// stream.  One tile per CTA: with more tiles than SMs two CTAs share one, each with half the slots.  Where tiles are few, the CTAs of a cluster take
+// consecutive parts of K; when all of them have finished their products, each writes its partial sums into the ring of the CTA that owns the output rows
+// (distributed shared memory, which takes about 13 bytes a cycle, so 128 rows cost three times what 32 do), and that adds them in the order of K.
+// 32 rows, bf16 out: 12288 x 4096 9.2 us (3.1 TB/s of weights; start, first loads and epilogue are half of it), 37888 x 3584 14.3 us (5.3 TB/s),
+// 126464 x 4096 51 us (5.7 TB/s, 0.87 of the copy rate); 128 rows 64 us.
 constexpr int ST_THREADS = 192;                  // TMA, MMA, four epilogue warps
 constexpr int ST_MAX_STAGES = 8;
 __host__ __device__ constexpr uint32_t st_stage_bytes(int T, int fmt) { return 128 * 128 + T * 128 + 2 * scale_blocks(fmt) * BLOCK_BYTES; }
-__host__ __device__ constexpr uint32_t st_exchange_bytes(int T) { return 128 * T * 4; }
-__host__ __device__ constexpr int st_stages(int T, int fmt) {
-    const int n = (int)((225 * 1024 - 1024 - st_exchange_bytes(T)) / st_stage_bytes(T, fmt));
+// ring slots of a CTA, one or two of which share an SM
+__host__ __device__ constexpr int st_stages(int T, int fmt, int per_sm) {
+    const int n = (int)(((per_sm == 1 ? 225 : 112) * 1024 - 1024) / st_stage_bytes(T, fmt));
     return n < ST_MAX_STAGES ? n : ST_MAX_STAGES;
 }
-__host__ __device__ constexpr size_t st_smem_bytes(int T, int fmt) { return 1024 + (size_t)st_stages(T, fmt) * st_stage_bytes(T, fmt) + st_exchange_bytes(T); }
+__host__ __device__ constexpr size_t st_smem_bytes(int T, int fmt, int per_sm) { return 1024 + (size_t)st_stages(T, fmt, per_sm) * st_stage_bytes(T, fmt); }
+static_assert(st_stages(128, NV, 1) * st_stage_bytes(128, NV) >= 128 * 128 * 4 && st_stages(32, NV, 1) * st_stage_bytes(32, NV) >= 128 * 32 * 4, "the ring takes the partial sums");
 
 template <int T, int FMT, typename OUT>
-__global__ void __launch_bounds__(ST_THREADS, 1)
+__global__ void __launch_bounds__(ST_THREADS, 2)
 gemm_stream_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ GemmArgs g) {
     extern __shared__ uint8_t smem_raw[];
-    __shared__ uint64_t bars[2 * ST_MAX_STAGES + 1];
+    __shared__ uint64_t bars[2 * ST_MAX_STAGES + 2];
     __shared__ uint32_t tmem_base_sh;
     __shared__ int abort_sh;
-    constexpr int STAGES = st_stages(T, FMT), SB = scale_blocks(FMT);
+    constexpr int SB = scale_blocks(FMT);
+    const int STAGES = g.stages;
     constexpr uint32_t STAGE = st_stage_bytes(T, FMT);
     constexpr uint32_t A_OFF = 128 * 128, BS_OFF = A_OFF + T * 128, AS_OFF = BS_OFF + SB * BLOCK_BYTES;
     constexpr uint32_t COLS = 256, SF_COL = 128;          // accumulator: columns 0 .. T - 1; two sets of scales from column 128 on
@@ -103,6 +108,7 @@ gemm_stream_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
     if (threadIdx.x == 0) {
         for (int s = 0; s < STAGES; ++s) { mbar_init(full(s), 1); mbar_init(empty(s), 1); }
         mbar_init(done, 1);
+        mbar_init(done + 8u, 1);
         abort_sh = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -113,8 +119,6 @@ gemm_stream_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
     tc_fence_after();
     pdl_trigger();
     const uint32_t tmem = tmem_base_sh;
-    // (every CTA of the cluster runs before another one writes into its shared memory)
-    if (g.split > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
 
     int issued = 0;                                       // ring slots that this thread has asked for
     if (warp == 0) {
@@ -166,8 +170,8 @@ gemm_stream_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
     // ---- epilogue: tensor-memory lane = output column, accumulator column = output row ----
     const int quarter = warp & 3;
     const uint32_t lane_base = tmem + ((uint32_t)(quarter * 32) << 16);
-    const int rows_each = T / g.split;                    // output rows that this CTA finishes
-    float* ex = reinterpret_cast<float*>(smem + (size_t)STAGES * STAGE);
+    const int rows_each = T / g.split;                    // output rows that this CTA finishes (a power of two)
+    const int live = min(T, g.M - tile_m * T);            // rows of the tile that exist
     bool ok = true;
     if (warp >= 2) {
         ok = mbar_wait(done, 0, abort_flag) && !*abort_flag;
@@ -186,37 +190,58 @@ gemm_stream_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
     };
     if (g.split == 1) {
         if (warp >= 2)
-            for (int c = 0; c < T; c += 16) {
+#pragma unroll 1
+            for (int c = 0; c < live; c += 16) {
                 float v[16];
                 tmem_ld16(lane_base + (uint32_t)c, v);
 #pragma unroll
                 for (int i = 0; i < 16; ++i) store(tile_m * T + c + i, v[i]);
             }
     } else {
-        asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
-        if (warp >= 2)
-            for (int c = 0; c < T; c += 16) {
-                float v[16];
-                tmem_ld16(lane_base + (uint32_t)c, v);
-                if (kb0 >= kb1 || !ok) {
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) v[i] = ok ? 0.f : __uint_as_float(0x7fc00000u);
-                }
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const int owner = (c + i) / rows_each, at = (c + i) - owner * rows_each;
-                    const uint32_t dst = dsmem_addr(smem_u32(ex + (rank * rows_each + at) * 128 + quarter * 32 + lane), (uint32_t)owner);
-                    asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(dst), "f"(v[i]) : "memory");
-                }
-            }
+        // (the products of every CTA have completed: their operands' place is free)
+        if (warp == 2 && !ok && lane < g.split) asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(dsmem_addr(smem_u32(&abort_sh), (uint32_t)lane)), "r"(1u) : "memory");
         __syncwarp();
         cluster_sync_all();
-        if (warp >= 2)
-            for (int i = 0; i < rows_each; ++i) {
-                float v = 0.f;
-                for (int s = 0; s < g.split; ++s) v += ex[(s * rows_each + i) * 128 + quarter * 32 + lane];
-                store(tile_m * T + rank * rows_each + i, v);
+        const int col = quarter * 32 + lane;
+        if (warp >= 2) {
+            const int shift = __ffs(rows_each) - 1;
+            const uint32_t mine = smem_base + (uint32_t)((rank * (rows_each >> 2) * 128 + col) * 16);
+#pragma unroll 1
+            for (int c = 0; c < live; c += 16) {
+                float v[16];
+                tmem_ld16(lane_base + (uint32_t)c, v);
+#pragma unroll
+                for (int i = 0; i < 16; i += 4) {
+                    const uint32_t dst = dsmem_addr(mine + (uint32_t)((c + i) & (rows_each - 1)) * 512u, (uint32_t)((c + i) >> shift));
+                    asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(dst), "f"(v[i]), "f"(v[i + 1]), "f"(v[i + 2]), "f"(v[i + 3]) : "memory");
+                }
             }
+        }
+        __syncwarp();
+        cluster_sync_all();
+        if (warp >= 2) {
+            if (*abort_flag) scale = __uint_as_float(0x7fc00000u);
+            OUT* dst = (OUT*)g.out + (size_t)(tile_m * T + rank * rows_each) * g.ld + n;
+            const uint32_t from = smem_base + (uint32_t)(col * 16), step = (uint32_t)rows_each * 512u;
+            const int rows = min(rows_each, live - rank * rows_each);
+            for (int i = 0; i < rows; i += 4) {           // (rows_each is 4 or more)
+                float x[8][4];
+#pragma unroll
+                for (int s = 0; s < 8; ++s) {             // all loads at once; -0: adds nothing
+                    x[s][0] = x[s][1] = x[s][2] = x[s][3] = -0.f;
+                    if (s < g.split)
+                        asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(x[s][0]), "=f"(x[s][1]), "=f"(x[s][2]), "=f"(x[s][3])
+                                     : "r"(from + (uint32_t)s * step + (uint32_t)i * 512u) : "memory");
+                }
+#pragma unroll
+                for (int s = 1; s < 8; ++s)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) x[0][j] += x[s][j];
+#pragma unroll
+                for (int j = 0; j < 4; ++j, dst += g.ld)
+                    if (i + j < rows && n < g.N) *dst = from_f<OUT>(x[0][j] * scale);
+            }
+        }
     }
     tc_fence_before();
     __syncthreads();

@@ -23,22 +23,34 @@ using namespace ps;
 
 // Environment switches: read by the first call and by polestar_reload_env, never on the launch path.
 //   POLESTAR_KV4_KERNEL (0 = automatic): 1 the warp-level attention kernel, 2 the tensor-core one where it applies (used by the tests)
-static std::atomic<int> g_kv4_kernel{-1};
-namespace ps { void reload_operator_switches() { const char* e = getenv("POLESTAR_KV4_KERNEL"); g_kv4_kernel.store(e ? atoi(e) : 0); } }
-static int switch_kv4() {
-    if (g_kv4_kernel.load() < 0) reload_operator_switches();
-    return g_kv4_kernel.load();
+//   POLESTAR_FP4_KERNEL (0 = automatic): 1 the product's kernel for few rows, 2 the one for many (used by the tests)
+static std::atomic<int> g_kv4_kernel{-1}, g_fp4_kernel{-1};
+namespace ps {
+void reload_operator_switches() {
+    const char *kv = getenv("POLESTAR_KV4_KERNEL"), *fp = getenv("POLESTAR_FP4_KERNEL");
+    g_kv4_kernel.store(kv ? std::max(0, atoi(kv)) : 0);
+    g_fp4_kernel.store(fp ? std::max(0, atoi(fp)) : 0);
+}
+}
+static int read_switch(const std::atomic<int>& s) {
+    if (s.load() < 0) reload_operator_switches();
+    return s.load();
 }
 
 // Facts of the CURRENT device; the first call on a device queries them and raises the shared-memory limits of the kernels that need
 // more than the default there (function attributes are per device).
-struct DevInfo { bool ready = false; int sm_count = 0; int gemm_pairs = 0; };      // CTA pairs of the product that are resident at once
+struct DevInfo {
+    bool ready = false;
+    int sm_count = 0;
+    int gemm_pairs = 0;                          // CTA pairs of the product for many rows that are resident at once ...
+    int clusters[3] = {};                        // ... and clusters of 2, 4 and 8 CTAs of the one for few
+};
 static const int MAX_DEVICES = 64;
 static std::mutex g_mu;
 static DevInfo g_dev[MAX_DEVICES];
 namespace ps { void note_sm_count(int n); }               // polestar.cu: what polestar_sm_count() answers
 static cudaError_t set_kernel_attributes();
-static int resident_gemm_pairs(int sms);
+static void resident_clusters(DevInfo* di);
 static int device_info(DevInfo* out) {
     int dev = 0;
     CK(cudaGetDevice(&dev));
@@ -48,7 +60,7 @@ static int device_info(DevInfo* out) {
     if (!di.ready) {
         CK(cudaDeviceGetAttribute(&di.sm_count, cudaDevAttrMultiProcessorCount, dev));
         CK(set_kernel_attributes());
-        di.gemm_pairs = resident_gemm_pairs(di.sm_count);
+        resident_clusters(&di);
         di.ready = true;
     }
     note_sm_count(di.sm_count);
@@ -174,27 +186,42 @@ static int launch_gemm_pair(const uint8_t* a, const uint8_t* b, fp4::GemmArgs g,
 }
 
 template <int T, int FMT, typename OUT>
-static int launch_gemm_stream(const uint8_t* a, const uint8_t* b, fp4::GemmArgs g, int sms, cudaStream_t st) {
+static int launch_gemm_stream(const uint8_t* a, const uint8_t* b, fp4::GemmArgs g, const DevInfo& di, cudaStream_t st) {
     CUtensorMap ma, mb;
     if (!make_code_map(&ma, a, g.M, g.K / 2, T) || !make_code_map(&mb, b, g.N, g.K / 2, 128)) return POLESTAR_E_CUDA;
     const long long tiles_n = ((long long)g.N + 127) / 128, tiles_m = ((long long)g.M + T - 1) / T;
     const int kbs = (g.K + fp4::KB - 1) / fp4::KB;
-    // a cluster over K while its CTAs have an SM each and two slots' worth of K
+    // The CTAs of a cluster share K while all clusters run at once and each has two slots of K: a slot takes 0.4 us, handing the sums over 1.0 us and 0.016 us a row.  (us,
+    // not split / split in 2, 4, 8: 1 row, 1024 x 4096 8.5 / 6.3, 4.7, 4.1; 128 rows, 1024 x 4096 9.5 / 9.1, 7.5, 7.3; 128 rows, 512 x 1024 4.5 / 6.6.)
     g.split = 1;
-    while (g.split < 8 && tiles_n * tiles_m * g.split * 2 <= sms && g.split * 4 <= kbs) g.split *= 2;
+    double least = 0.4 * kbs;
+    for (int i = 0; i < 3 && tiles_n * tiles_m <= di.clusters[i] && 4 << i <= kbs; ++i) {
+        const double us = 0.4 * kbs / (2 << i) + 1.0 + 0.016 * std::min(T, g.M);
+        if (us < least) { least = us; g.split = 2 << i; }
+    }
     if (tiles_m > 65535 || tiles_n * g.split > INT32_MAX) return POLESTAR_E_INVAL;
     const dim3 grid((unsigned)(tiles_n * g.split), (unsigned)tiles_m);
-    const size_t smem = fp4::st_smem_bytes(T, FMT);
+    // more tiles than SMs: two CTAs on each, with half the slots, so that one's start and end pass under the other's stream (us, one / two: 32 rows,
+    // 37888 x 3584 19.7 / 14.3, 126464 x 4096 69.5 / 51.2; 128 rows, 126464 x 4096 93 / 64)
+    const int per_sm = tiles_n * tiles_m > di.sm_count ? 2 : 1;
+    const size_t smem = fp4::st_smem_bytes(T, FMT, per_sm);
+    g.stages = fp4::st_stages(T, FMT, per_sm);
     if (g.split > 1) CK(launch_k_cluster(fp4::gemm_stream_kernel<T, FMT, OUT>, grid, dim3(fp4::ST_THREADS), smem, st, (unsigned)g.split, ma, mb, g));
     else CK(launch_k(fp4::gemm_stream_kernel<T, FMT, OUT>, grid, dim3(fp4::ST_THREADS), smem, st, ma, mb, g));
     return POLESTAR_OK;
 }
+// Which kernel: the one for few rows up to 128 of them, and beyond while its tiles of 128 x 128 run at once, one to an SM, or two where the pairs' tiles of
+// 256 x 256 would take two rounds.  us, few / many: 128 rows, 37888 x 3584 15.9 / 24.2; 256 rows, 4096 x 12288 16.7 / 24.8; 512 rows, 4096 x 4096 10.4 /
+// 11.8 (128 tiles), 1024 rows 12.4 / 12.6 (256); 384 rows, 12288 x 4096 13.0 / 20.4 (288), 512 rows 22.3 / 20.4 (384).
 template <int FMT, typename OUT>
-static int launch_gemm_fp4(const uint8_t* a, const uint8_t* b, const fp4::GemmArgs& g, int sms, int pairs, cudaStream_t st) {
-    if (pairs > 0 && g.M > 128) return launch_gemm_pair<FMT, OUT>(a, b, g, pairs, st);
-    if (g.M <= 32) return launch_gemm_stream<32, FMT, OUT>(a, b, g, sms, st);
-    if (g.M <= 64) return launch_gemm_stream<64, FMT, OUT>(a, b, g, sms, st);
-    return launch_gemm_stream<128, FMT, OUT>(a, b, g, sms, st);
+static int launch_gemm_fp4(const uint8_t* a, const uint8_t* b, const fp4::GemmArgs& g, const DevInfo& di, cudaStream_t st) {
+    auto tiles = [&](long long size) { return ((g.M + size - 1) / size) * ((g.N + size - 1) / size); };
+    const int forced = read_switch(g_fp4_kernel);
+    const bool few = g.M <= 128 || tiles(128) <= di.sm_count || (tiles(128) <= 2 * di.sm_count && tiles(fp4::PR_TILE) > di.gemm_pairs);
+    if (di.gemm_pairs > 0 && (forced ? forced == 2 : !few)) return launch_gemm_pair<FMT, OUT>(a, b, g, di.gemm_pairs, st);
+    if (g.M <= 32) return launch_gemm_stream<32, FMT, OUT>(a, b, g, di, st);
+    if (g.M <= 64) return launch_gemm_stream<64, FMT, OUT>(a, b, g, di, st);
+    return launch_gemm_stream<128, FMT, OUT>(a, b, g, di, st);
 }
 
 extern "C" int polestar_k_fp4_matmul(const uint8_t* a_codes, const uint8_t* a_scales, const uint8_t* b_codes, const uint8_t* b_scales,
@@ -215,8 +242,8 @@ extern "C" int polestar_k_fp4_matmul(const uint8_t* a_codes, const uint8_t* a_sc
     cudaStream_t st = (cudaStream_t)stream;
     const bool nv = format == POLESTAR_FP4_NV;
     if (out_dtype == POLESTAR_BF16)
-        return nv ? launch_gemm_fp4<fp4::NV, __nv_bfloat16>(a_codes, b_codes, g, di.sm_count, di.gemm_pairs, st) : launch_gemm_fp4<fp4::MX, __nv_bfloat16>(a_codes, b_codes, g, di.sm_count, di.gemm_pairs, st);
-    return nv ? launch_gemm_fp4<fp4::NV, float>(a_codes, b_codes, g, di.sm_count, di.gemm_pairs, st) : launch_gemm_fp4<fp4::MX, float>(a_codes, b_codes, g, di.sm_count, di.gemm_pairs, st);
+        return nv ? launch_gemm_fp4<fp4::NV, __nv_bfloat16>(a_codes, b_codes, g, di, st) : launch_gemm_fp4<fp4::MX, __nv_bfloat16>(a_codes, b_codes, g, di, st);
+    return nv ? launch_gemm_fp4<fp4::NV, float>(a_codes, b_codes, g, di, st) : launch_gemm_fp4<fp4::MX, float>(a_codes, b_codes, g, di, st);
 }
 
 // A cache of keys and values in 4 bits: what append and attention accept of its geometry.
@@ -240,10 +267,16 @@ extern "C" int polestar_k_kv4_append(const void* k, const void* v, const int32_t
     fp4::AppendArgs a;
     a.x[0] = k; a.x[1] = v; a.deq[0] = k_deq; a.deq[1] = v_deq; a.codes[0] = kc; a.codes[1] = vc; a.scales[0] = ks; a.scales[1] = vs;
     a.t[0] = k_scale; a.t[1] = v_scale; a.idx = idx; a.counts = count; a.R = R; a.cap = cap; a.width = n_kv * head_dim;
-    // rows of a block: four rounds of loads' worth, so that a long list is not scanned by every row, while there are blocks for all SMs
+    // rows of a block: two rounds of loads' worth while there are eight blocks for every SM; more, and fewer blocks, where the list is longer than what a block
+    // writes, since each looks through the rest of it
     const int pieces = a.width / (dtype == POLESTAR_BF16 ? 8 : 4);
     int rpb = std::max(1, fp4::THREADS / pieces);
-    while (rpb * 2 <= fp4::APPEND_MAX_ROWS && rpb * pieces < 8 * fp4::THREADS && 2LL * batch * ((R + 2 * rpb - 1) / (2 * rpb)) >= 8LL * di.sm_count) rpb *= 2;
+    while (rpb * 2 <= fp4::APPEND_MAX_ROWS) {
+        const bool longer = idx && R > rpb * pieces;
+        if (!longer && rpb * pieces >= 8 * fp4::THREADS) break;
+        if (2LL * batch * ((R + 2 * rpb - 1) / (2 * rpb)) < (longer ? 3LL : 8LL) * di.sm_count) break;
+        rpb *= 2;
+    }
     a.rows_per_block = std::min(rpb, fp4::APPEND_MAX_ROWS);
     const dim3 grid((R + a.rows_per_block - 1) / a.rows_per_block, batch, 2);
     if (dtype == POLESTAR_BF16) CK(launch_k(fp4::kv_append_kernel<__nv_bfloat16>, grid, dim3(fp4::THREADS), 0, (cudaStream_t)stream, a));
@@ -304,7 +337,7 @@ static Kv4Tc kv4_tc_plan(long long batch, long long R, int cap, int n_heads, int
 // heads 40 / 19; 896 rows, 65536 keys x 4 heads 650 / 156.
 static bool kv4_use_tc(int dtype, int head_dim, const Kv4Warp& w, const Kv4Tc& t, long long batch, int cap, int n_kv) {
     if (dtype != POLESTAR_BF16 || head_dim != kv4::TC_DH) return false;
-    const int forced = switch_kv4();
+    const int forced = read_switch(g_kv4_kernel);
     if (forced) return forced == 2;
     const double ctas = (double)w.slots * n_kv * w.tiles, part = std::ceil((double)((cap + 127) / 128) * batch / w.slots);
     const double all = (double)batch * n_kv * w.tiles * ((cap + 127) / 128);
@@ -417,7 +450,7 @@ extern "C" int polestar_k_token_logprobs(const void* logits, int64_t ld, int32_t
 // kernels with more shared memory than the default limit
 template <int T, int FMT>
 static cudaError_t stream_attributes() {
-    const int n = (int)fp4::st_smem_bytes(T, FMT);
+    const int n = (int)fp4::st_smem_bytes(T, FMT, 1);
     cudaError_t e = cudaFuncSetAttribute(fp4::gemm_stream_kernel<T, FMT, float>, cudaFuncAttributeMaxDynamicSharedMemorySize, n);
     if (e == cudaSuccess) e = cudaFuncSetAttribute(fp4::gemm_stream_kernel<T, FMT, __nv_bfloat16>, cudaFuncAttributeMaxDynamicSharedMemorySize, n);
     return e;
@@ -429,16 +462,21 @@ static cudaError_t pair_attributes() {
     if (e == cudaSuccess) e = cudaFuncSetAttribute(fp4::gemm_pair_kernel<FMT, __nv_bfloat16>, cudaFuncAttributeMaxDynamicSharedMemorySize, n);
     return e;
 }
-static int resident_gemm_pairs(int sms) {
+static int resident(const void* kernel, int cluster, int threads, size_t smem, int sms) {
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(2 * sms); cfg.blockDim = dim3(fp4::PR_THREADS); cfg.dynamicSmemBytes = fp4::pr_smem_bytes(fp4::NV);
+    cfg.gridDim = dim3(cluster * sms); cfg.blockDim = dim3(threads); cfg.dynamicSmemBytes = smem;
     cudaLaunchAttribute at[1];
     at[0].id = cudaLaunchAttributeClusterDimension;
-    at[0].val.clusterDim.x = 2; at[0].val.clusterDim.y = 1; at[0].val.clusterDim.z = 1;
+    at[0].val.clusterDim.x = cluster; at[0].val.clusterDim.y = 1; at[0].val.clusterDim.z = 1;
     cfg.attrs = at; cfg.numAttrs = 1;
     int n = 0;
-    if (cudaOccupancyMaxActiveClusters(&n, fp4::gemm_pair_kernel<fp4::NV, __nv_bfloat16>, &cfg) != cudaSuccess) { cudaGetLastError(); return 0; }
+    if (cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) != cudaSuccess) { cudaGetLastError(); return 0; }
     return n;
+}
+static void resident_clusters(DevInfo* di) {
+    di->gemm_pairs = resident((const void*)fp4::gemm_pair_kernel<fp4::NV, __nv_bfloat16>, 2, fp4::PR_THREADS, fp4::pr_smem_bytes(fp4::NV), di->sm_count);
+    for (int i = 0; i < 3; ++i)
+        di->clusters[i] = resident((const void*)fp4::gemm_stream_kernel<128, fp4::NV, __nv_bfloat16>, 2 << i, fp4::ST_THREADS, fp4::st_smem_bytes(128, fp4::NV, 1), di->sm_count);
 }
 static cudaError_t set_kernel_attributes() {
     cudaError_t e;

@@ -55,6 +55,19 @@ def test_products_of_many_rows(M, N, K, dtype, fmt):
     check(M, N, K, fmt, dtype, seed=7)
 
 
+@pytest.mark.parametrize("kernel", [1, 2])
+@pytest.mark.parametrize("M,N,K,dtype", [
+    (1, 1, 64, torch.float32), (7, 130, 448, torch.bfloat16), (128, 300, 2304, torch.float32),          # one row tile; K split in two, four, eight
+    (64, 128, 4096, torch.float32), (20, 900, 8192, torch.bfloat16), (130, 400, 4160, torch.float32), (300, 520, 960, torch.bfloat16),
+    (257, 1255, 1088, torch.float32), (100, 20100, 320, torch.bfloat16), (513, 9000, 448, torch.float32), (1000, 1100, 2048, torch.bfloat16),
+])
+def test_both_kernels(monkeypatch, kernel, M, N, K, dtype):
+    monkeypatch.setenv("POLESTAR_FP4_KERNEL", str(kernel))
+    Bd.polestar_reload_env()
+    check(M, N, K, F.NV, dtype, ld=N + 3, seed=11)
+    check(M, N, K, F.MX, dtype, seed=12)
+
+
 @pytest.mark.parametrize("fmt", [F.NV, F.MX])
 @pytest.mark.parametrize("M,N,K,pad", [(5, 131, 128, 3), (70, 515, 1088, 1), (260, 250, 512, 6)])
 def test_products_in_bf16_with_strided_rows(M, N, K, pad, fmt):
