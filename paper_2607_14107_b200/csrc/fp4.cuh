@@ -8,8 +8,8 @@
 // A group with an infinity or NaN gets the scale NaN (0x7f / 0xff) and zero codes: what reads it sees NaN in all of the group.  A group
 // whose scale rounds to zero is zero.  All decisions are float32 with IEEE division.
 //
-// Bound by the copy at thousands of rows, by latency at a block of rows.  A lane holds 16 bytes of a row (4 or 8 channels), so every
-// load and store of a warp is contiguous whatever the type; the lanes of a group find its maximum by shuffles.
+// Bound by the copy at thousands of rows of fp32, by instructions at thousands of rows of bf16, by latency at a block of rows.  A lane holds 32 bytes of a row
+// (8 or 16 channels); the lanes of a group find its maximum by shuffles.
 #pragma once
 #include <cuda_fp16.h>
 #include <climits>
@@ -110,53 +110,71 @@ template <> struct Vec<__nv_bfloat16> {
     }
 };
 
-// One lane's 16 bytes of a group (all lanes of the warp take part; the lanes of a group are neighbours): the codes, four bits each, channel
-// 0 lowest, the group's scale byte, and the stored values in the row's type.  The conversion to E2M1 rounds to nearest, ties to the even code, and
-// saturates; groups whose unit s t is so far out that the division's steps could overflow or underflow divide by the instruction.
+// One lane's piece of a row: 32 bytes of it, a group's worth or less, so that what a group costs once (its maximum, scale and reciprocal) is paid by as few
+// lanes as may be.  All lanes of the warp take part; the lanes of a group are neighbours.  Results: the codes, four bits each, channel 0 lowest, the group's
+// scale byte, and the stored values in the row's type.  The conversion to E2M1 rounds to nearest, ties to the even code, and saturates; groups whose
+// unit s t is so far out that the division's steps could overflow or underflow divide by the instruction.
+template <typename T> struct Piece {
+    static constexpr int N = 2 * Vec<T>::N, WORDS = N / 8;                 // channels, words of codes
+    uint4 w[2];
+    __device__ __forceinline__ void clear() { w[0] = w[1] = make_uint4(0u, 0u, 0u, 0u); }
+    __device__ __forceinline__ void load(const uint4* p) { w[0] = __ldg(p); w[1] = __ldg(p + 1); }
+};
 template <typename T, int FMT>
-__device__ __forceinline__ uint32_t encode(const uint4& w, const Factor& f, uint32_t* byte, uint4* stored) {
-    constexpr int N = Vec<T>::N, LANES = group(FMT) / N;
-    uint32_t am = Vec<T>::amax(w);
+__device__ __forceinline__ void encode(const Piece<T>& x, const Factor& f, uint32_t (&codes)[Piece<T>::WORDS], uint32_t* byte, Piece<T>* stored) {
+    constexpr int N = Piece<T>::N, LANES = group(FMT) / N, H = Vec<T>::N;
+    uint32_t am = max(Vec<T>::amax(x.w[0]), Vec<T>::amax(x.w[1]));
 #pragma unroll
     for (int o = 1; o < LANES; o <<= 1) am = max(am, __shfl_xor_sync(0xffffffffu, am, o));
     const float s = group_scale<FMT>(am, f, byte);
     const float u = __fmul_rn(s, f.t);
     float v[N];
-    Vec<T>::unpack(w, v);
-    uint32_t codes = 0;
+    Vec<T>::unpack(x.w[0], v);
+    Vec<T>::unpack(x.w[1], v + H);
+#pragma unroll
+    for (int h = 0; h < Piece<T>::WORDS; ++h) codes[h] = 0u;
     if (__builtin_expect(in_range(u), 1)) {
         const float r = __frcp_rn(u);
         const uint64_t r2 = f2_pack(r, r), nu = f2_pack(-u, -u);
-        uint32_t c[4] = {0, 0, 0, 0};
 #pragma unroll
-        for (int i = 0; i < N / 2; ++i) {
-            const uint64_t x = f2_pack(v[2 * i], v[2 * i + 1]), q = f2_mul(x, r2);
-            float y0, y1;
-            f2_unpack(f2_fma(f2_fma(nu, q, x), r2, q), y0, y1);
-            asm("{\n .reg .b8 b;\n cvt.rn.satfinite.e2m1x2.f32 b, %2, %1;\n mov.b32 %0, {b, 0, 0, 0};\n}\n" : "=r"(c[i]) : "f"(y0), "f"(y1));
+        for (int h = 0; h < Piece<T>::WORDS; ++h) {
+            float y[8];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const uint64_t z = f2_pack(v[8 * h + 2 * i], v[8 * h + 2 * i + 1]), q = f2_mul(z, r2);
+                f2_unpack(f2_fma(f2_fma(nu, q, z), r2, q), y[2 * i], y[2 * i + 1]);
+            }
+            asm("{\n .reg .b8 a, b, c, d;\n cvt.rn.satfinite.e2m1x2.f32 a, %2, %1;\n cvt.rn.satfinite.e2m1x2.f32 b, %4, %3;\n"
+                " cvt.rn.satfinite.e2m1x2.f32 c, %6, %5;\n cvt.rn.satfinite.e2m1x2.f32 d, %8, %7;\n mov.b32 %0, {a, b, c, d};\n}\n"
+                : "=r"(codes[h]) : "f"(y[0]), "f"(y[1]), "f"(y[2]), "f"(y[3]), "f"(y[4]), "f"(y[5]), "f"(y[6]), "f"(y[7]));
         }
-        codes = c[0] | (c[1] << 8) | (c[2] << 16) | (c[3] << 24);
     } else if (s > 0.f) {
 #pragma unroll
-        for (int i = 0; i < N; ++i) codes |= e2m1_code(v[i], u) << (4 * i);
+        for (int i = 0; i < N; ++i) codes[i >> 3] |= e2m1_code(v[i], u) << (4 * (i & 7));
     }
     if (stored) {
-        uint32_t h[4];
-        asm("{\n .reg .b8 a, b, c, d;\n mov.b32 {a, b, c, d}, %4;\n cvt.rn.f16x2.e2m1x2 %0, a;\n cvt.rn.f16x2.e2m1x2 %1, b;\n"
-            " cvt.rn.f16x2.e2m1x2 %2, c;\n cvt.rn.f16x2.e2m1x2 %3, d;\n}\n" : "=r"(h[0]), "=r"(h[1]), "=r"(h[2]), "=r"(h[3]) : "r"(codes));
         const uint64_t s2 = f2_pack(s, s), t2 = f2_pack(f.t, f.t);
 #pragma unroll
-        for (int i = 0; i < N / 2; ++i) {
-            const float2 g = __half22float2(*reinterpret_cast<const __half2*>(&h[i]));
-            f2_unpack(f2_mul(f2_mul(f2_pack(g.x, g.y), s2), t2), v[2 * i], v[2 * i + 1]);
+        for (int k = 0; k < Piece<T>::WORDS; ++k) {
+            uint32_t h[4];
+            asm("{\n .reg .b8 a, b, c, d;\n mov.b32 {a, b, c, d}, %4;\n cvt.rn.f16x2.e2m1x2 %0, a;\n cvt.rn.f16x2.e2m1x2 %1, b;\n"
+                " cvt.rn.f16x2.e2m1x2 %2, c;\n cvt.rn.f16x2.e2m1x2 %3, d;\n}\n" : "=r"(h[0]), "=r"(h[1]), "=r"(h[2]), "=r"(h[3]) : "r"(codes[k]));
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float2 g = __half22float2(*reinterpret_cast<const __half2*>(&h[i]));
+                f2_unpack(f2_mul(f2_mul(f2_pack(g.x, g.y), s2), t2), v[8 * k + 2 * i], v[8 * k + 2 * i + 1]);
+            }
         }
-        *stored = Vec<T>::pack(v);
+        stored->w[0] = Vec<T>::pack(v);
+        stored->w[1] = Vec<T>::pack(v + H);
     }
-    return codes;
 }
-template <typename T> __device__ __forceinline__ void store_codes(uint8_t* p, uint32_t c);
-template <> __device__ __forceinline__ void store_codes<float>(uint8_t* p, uint32_t c) { *reinterpret_cast<uint16_t*>(p) = (uint16_t)c; }
-template <> __device__ __forceinline__ void store_codes<__nv_bfloat16>(uint8_t* p, uint32_t c) { *reinterpret_cast<uint32_t*>(p) = c; }
+// (codes are 4-byte aligned)
+__device__ __forceinline__ void store_codes(uint8_t* p, const uint32_t (&c)[1]) { *reinterpret_cast<uint32_t*>(p) = c[0]; }
+__device__ __forceinline__ void store_codes(uint8_t* p, const uint32_t (&c)[2]) {
+    if (((uintptr_t)p & 7) == 0) *reinterpret_cast<uint2*>(p) = make_uint2(c[0], c[1]);
+    else { reinterpret_cast<uint32_t*>(p)[0] = c[0]; reinterpret_cast<uint32_t*>(p)[1] = c[1]; }
+}
 
 struct QuantArgs {
     const void* x; long long ld_x;       // rows, elements between them
@@ -167,37 +185,44 @@ struct QuantArgs {
     int d, layout;
 };
 
-// Pieces of 16 bytes: piece i of the call is piece i % ppr of row i / ppr.  A block takes PER x THREADS consecutive ones, all loads of a
-// thread in flight at once.
+// Piece i of the call is piece i % ppr of row i / ppr.  A block takes PER x THREADS consecutive ones, all loads of a thread in flight at once.
 template <typename T, int FMT, int PER>
 __global__ void __launch_bounds__(THREADS) quantize_kernel(const __grid_constant__ QuantArgs a) {
     KERNEL_PROLOGUE(20);   // fp4 quantize_kernel
-    constexpr int N = Vec<T>::N, G = group(FMT);
+    constexpr int N = Piece<T>::N, G = group(FMT);
     const int ppr = a.d / N, groups = a.d / G, g4 = (groups + 3) >> 2;
     const Factor t = make_factor<FMT>(a.t);
     const long long first = (long long)blockIdx.x * (PER * THREADS), total = a.rows * ppr;
     const long long row0 = first / ppr;
     const unsigned rem0 = (unsigned)(first - row0 * ppr);
-    uint4 w[PER];
+    // quotients of numbers below ppr + PER * THREADS by ppr: 0 or 1 where ppr is that large, else a product with the rounded-up reciprocal (numbers and
+    // divisor below 2^12: exact)
+    const bool wide = ppr >= PER * THREADS;
+    const unsigned inv = 0xffffffffu / (unsigned)ppr + 1u;                 // (ppr is 2 or more)
+    Piece<T> x[PER];
     long long row[PER];
     int c[PER];
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
         const unsigned loc = rem0 + i * THREADS + threadIdx.x;
-        const unsigned dr = loc / (unsigned)ppr;
+        const unsigned dr = wide ? (loc >= (unsigned)ppr ? 1u : 0u) : __umulhi(loc, inv);
         row[i] = first + i * THREADS + threadIdx.x < total ? row0 + dr : -1;
         c[i] = (int)(loc - dr * ppr);
-        w[i] = make_uint4(0u, 0u, 0u, 0u);
-        if (row[i] >= 0) w[i] = __ldg(reinterpret_cast<const uint4*>((const T*)a.x + row[i] * a.ld_x) + c[i]);
+        x[i].clear();
+        if (row[i] >= 0) x[i].load(reinterpret_cast<const uint4*>((const T*)a.x + row[i] * a.ld_x) + 2 * c[i]);
     }
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
-        uint32_t byte;
-        uint4 stored;
-        const uint32_t codes = encode<T, FMT>(w[i], t, &byte, a.deq ? &stored : nullptr);
+        uint32_t byte, codes[Piece<T>::WORDS];
+        Piece<T> stored;
+        encode<T, FMT>(x[i], t, codes, &byte, a.deq ? &stored : nullptr);
         if (row[i] < 0) continue;
-        store_codes<T>(a.codes + row[i] * (a.d >> 1) + c[i] * (N / 2), codes);
-        if (a.deq) reinterpret_cast<uint4*>((T*)a.deq + row[i] * a.ld_deq)[c[i]] = stored;
+        store_codes(a.codes + row[i] * (a.d >> 1) + c[i] * (N / 2), codes);
+        if (a.deq) {
+            uint4* to = reinterpret_cast<uint4*>((T*)a.deq + row[i] * a.ld_deq) + 2 * c[i];
+            to[0] = stored.w[0];
+            to[1] = stored.w[1];
+        }
         const int g = c[i] * N / G;
         if (c[i] * N == g * G) {
             if (a.layout == ROWS) {
@@ -210,11 +235,16 @@ __global__ void __launch_bounds__(THREADS) quantize_kernel(const __grid_constant
             }
         }
     }
-    // tiled scales: rows that do not exist, up to the next 128, are zero
-    if (a.layout == TILED) {
-        const int pad = (int)(-a.rows & 127);
-        for (long long i = (long long)blockIdx.x * THREADS + threadIdx.x; i < (long long)pad * g4; i += (long long)gridDim.x * THREADS)
-            *reinterpret_cast<uint32_t*>(a.scales + tiled_offset(a.rows + i / g4, 4 * (int)(i % g4), g4)) = 0u;
+    // tiled scales: rows that do not exist, up to the next 128, are zero.  A warp takes a block, a lane the rows lane, lane + 32, + 64, + 96: 16 bytes
+    const int n = (int)(a.rows & 127);
+    if (a.layout == TILED && n != 0) {
+        const int lane = threadIdx.x & 31, k0 = max(0, (n - lane + 31) >> 5);
+        const bool whole = k0 == 0 && ((uintptr_t)a.scales & 15) == 0;
+        for (long long q = (long long)blockIdx.x * (THREADS / 32) + (threadIdx.x >> 5); q < g4; q += (long long)gridDim.x * (THREADS / 32)) {
+            uint32_t* at = reinterpret_cast<uint32_t*>(a.scales + ((a.rows >> 7) * g4 + q) * 512) + 4 * lane;
+            if (whole) *reinterpret_cast<uint4*>(at) = make_uint4(0u, 0u, 0u, 0u);
+            else for (int k = k0; k < 4; ++k) at[k] = 0u;
+        }
     }
 }
 
@@ -233,7 +263,7 @@ constexpr int APPEND_MAX_ROWS = 256;             // rows of a block
 template <typename T>
 __global__ void __launch_bounds__(THREADS) kv_append_kernel(const __grid_constant__ AppendArgs a) {
     KERNEL_PROLOGUE(21);   // fp4 kv_append_kernel
-    constexpr int N = Vec<T>::N;
+    constexpr int N = Piece<T>::N;
     __shared__ int pos[APPEND_MAX_ROWS];
     const int which = blockIdx.z;
     const size_t seq = blockIdx.y;
@@ -246,13 +276,14 @@ __global__ void __launch_bounds__(THREADS) kv_append_kernel(const __grid_constan
     }
     const int live = r1 - r0, ppr = a.width / N, total = live * ppr;
     const uint4* x = reinterpret_cast<const uint4*>((const T*)a.x[which] + (seq * a.R + r0) * a.width);
-    constexpr int PER = 4;
-    uint4 w[PER];
+    constexpr int PER = 2;
+    Piece<T> w[PER];
     auto load = [&](int b) {
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
             const int at = b + i * THREADS + threadIdx.x;
-            w[i] = at < total ? __ldg(x + at) : make_uint4(0u, 0u, 0u, 0u);
+            w[i].clear();
+            if (at < total) w[i].load(x + 2 * at);
         }
     };
     load(0);                                     // (under way while the list is looked through)
@@ -298,14 +329,14 @@ __global__ void __launch_bounds__(THREADS) kv_append_kernel(const __grid_constan
         for (int i = 0; i < PER; ++i) {
             if (b + i * THREADS >= total) break;     // (the same for all threads)
             const int at = b + i * THREADS + threadIdx.x;
-            uint32_t byte;
-            uint4 stored;
-            const uint32_t cd = encode<T, NV>(w[i], t, &byte, deq ? &stored : nullptr);
+            uint32_t byte, cd[Piece<T>::WORDS];
+            Piece<T> stored;
+            encode<T, NV>(w[i], t, cd, &byte, deq ? &stored : nullptr);
             if (at >= total) continue;
             const int r = at / ppr, c = at - r * ppr, p = pos[r];
-            if (deq) deq[at] = stored;
+            if (deq) { deq[2 * at] = stored.w[0]; deq[2 * at + 1] = stored.w[1]; }
             if (p < 0) continue;
-            store_codes<T>(codes + (size_t)p * (a.width >> 1) + c * (N / 2), cd);
+            store_codes(codes + (size_t)p * (a.width >> 1) + c * (N / 2), cd);
             if ((c * N) % 16 == 0) scales[(size_t)p * (a.width >> 4) + c * N / 16] = (uint8_t)byte;
         }
     }

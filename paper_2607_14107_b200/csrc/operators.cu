@@ -84,12 +84,12 @@ extern "C" size_t polestar_k_fp4_scale_bytes(int64_t rows, int32_t d, int32_t fo
 
 template <typename T, int FMT>
 static cudaError_t launch_quantize(const fp4::QuantArgs& a, int sms, cudaStream_t st) {
-    // One piece of 16 bytes per thread while that leaves SMs idle (a block of rows is latency), four where the loads have to be many:
-    const long long pieces = a.rows * (a.d / fp4::Vec<T>::N);
-    const bool deep = pieces >= 4LL * fp4::THREADS * 8 * sms;
-    const long long per = fp4::THREADS * (deep ? 4LL : 1LL), blocks = (pieces + per - 1) / per;
+    // one piece of 32 bytes per thread for few rows, two where the loads have to be many (us, one / two: 32 x 4096 bf16 2.3 / 2.6, 16384 x 4096 46 / 40, fp32 69 / 62)
+    const long long pieces = a.rows * (a.d / fp4::Piece<T>::N);
+    const bool deep = pieces >= 2LL * fp4::THREADS * 8 * sms;
+    const long long per = fp4::THREADS * (deep ? 2LL : 1LL), blocks = (pieces + per - 1) / per;
     if (blocks > INT32_MAX) return cudaErrorInvalidValue;
-    if (deep) return launch_k(fp4::quantize_kernel<T, FMT, 4>, dim3((unsigned)blocks), dim3(fp4::THREADS), 0, st, a);
+    if (deep) return launch_k(fp4::quantize_kernel<T, FMT, 2>, dim3((unsigned)blocks), dim3(fp4::THREADS), 0, st, a);
     return launch_k(fp4::quantize_kernel<T, FMT, 1>, dim3((unsigned)blocks), dim3(fp4::THREADS), 0, st, a);
 }
 
@@ -269,11 +269,11 @@ extern "C" int polestar_k_kv4_append(const void* k, const void* v, const int32_t
     a.t[0] = k_scale; a.t[1] = v_scale; a.idx = idx; a.counts = count; a.R = R; a.cap = cap; a.width = n_kv * head_dim;
     // rows of a block: two rounds of loads' worth while there are eight blocks for every SM; more, and fewer blocks, where the list is longer than what a block
     // writes, since each looks through the rest of it
-    const int pieces = a.width / (dtype == POLESTAR_BF16 ? 8 : 4);
+    const int pieces = a.width / (dtype == POLESTAR_BF16 ? fp4::Piece<__nv_bfloat16>::N : fp4::Piece<float>::N);
     int rpb = std::max(1, fp4::THREADS / pieces);
     while (rpb * 2 <= fp4::APPEND_MAX_ROWS) {
-        const bool longer = idx && R > rpb * pieces;
-        if (!longer && rpb * pieces >= 8 * fp4::THREADS) break;
+        const bool longer = idx && R > 2 * rpb * pieces;
+        if (!longer && rpb * pieces >= 4 * fp4::THREADS) break;
         if (2LL * batch * ((R + 2 * rpb - 1) / (2 * rpb)) < (longer ? 3LL : 8LL) * di.sm_count) break;
         rpb *= 2;
     }
