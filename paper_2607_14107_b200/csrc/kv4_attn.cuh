@@ -264,9 +264,13 @@ __global__ void __launch_bounds__(THREADS) kv4_attn_warp_kernel(const __grid_con
         const uint32_t st = ring + (uint32_t)slot * St::BYTES;
         slot = slot + 1 == DEPTH ? 0 : slot + 1;
         // scores of keys g and g + 8 (rows of the product) against rows 2t, 2t + 1
-        float s[NB][4];
+        // (the tensor core's sums lose their last places towards zero: fp32 rows keep the products of q's second term and of either half of the channels apart)
+        constexpr int SUMS = TERMS == 2 ? 3 : 1;
+        float s[NB][4], part_s[SUMS][NB][4];
 #pragma unroll
-        for (int n = 0; n < NB; ++n) s[n][0] = s[n][1] = s[n][2] = s[n][3] = 0.f;
+        for (int i = 0; i < SUMS; ++i)
+#pragma unroll
+            for (int n = 0; n < NB; ++n) part_s[i][n][0] = part_s[i][n][1] = part_s[i][n][2] = part_s[i][n][3] = 0.f;
         {
             uint32_t kw[2][DH / 32], ksc[2];
 #pragma unroll
@@ -297,10 +301,15 @@ __global__ void __launch_bounds__(THREADS) kv4_attn_warp_kernel(const __grid_con
 #pragma unroll
                     for (int n = 0; n < NB; ++n)
 #pragma unroll
-                        for (int tm = 0; tm < TERMS; ++tm) mma16816(s[n], fa, qf[tm][n][2 * w + y][0], qf[tm][n][2 * w + y][1]);
+                        for (int tm = 0; tm < TERMS; ++tm)
+                            mma16816(part_s[TERMS == 1 ? 0 : tm ? 2 : (2 * w + y) / (KS / 2)][n], fa, qf[tm][n][2 * w + y][0], qf[tm][n][2 * w + y][1]);
                 }
             }
         }
+#pragma unroll
+        for (int n = 0; n < NB; ++n)
+#pragma unroll
+            for (int x = 0; x < 4; ++x) s[n][x] = SUMS == 1 ? part_s[0][n][x] : (part_s[0][n][x] + part_s[SUMS / 2][n][x]) + part_s[SUMS - 1][n][x];
         bool grow = false;
         float y[NB][4];                          // score - m + LIFT
         if (__builtin_expect(j0 + CHUNK > hi, 0)) {
@@ -381,9 +390,17 @@ __global__ void __launch_bounds__(THREADS) kv4_attn_warp_kernel(const __grid_con
             for (int x = 0; x < 4; ++x) {
                 const uint32_t fa[4] = {h2mul(he[0][x], vs0), h2mul(ho[0][x], vs0), h2mul(he[1][x], vs1), h2mul(ho[1][x], vs1)};
 #pragma unroll
-                for (int n = 0; n < NB; ++n)
+                for (int n = 0; n < NB; ++n) {
+                    if (TERMS == 1) {
+                        mma16816(o[4 * w + x][n], fa, pf[0][n][0], pf[0][n][1]);
+                    } else {                     // (a chunk's sums by themselves, then rounded to nearest)
+                        float d[4] = {0.f, 0.f, 0.f, 0.f};
+                        mma16816(d, fa, pf[TERMS - 1][n][0], pf[TERMS - 1][n][1]);
+                        mma16816(d, fa, pf[0][n][0], pf[0][n][1]);
 #pragma unroll
-                    for (int tm = 0; tm < TERMS; ++tm) mma16816(o[4 * w + x][n], fa, pf[tm][n][0], pf[tm][n][1]);
+                        for (int z = 0; z < 4; ++z) o[4 * w + x][n][z] += d[z];
+                    }
+                }
             }
         }
     }
