@@ -9,7 +9,9 @@
 // whose scale rounds to zero is zero.  All decisions are float32 with IEEE division.
 //
 // Bound by the copy at thousands of rows of fp32, by instructions at thousands of rows of bf16, by latency at a block of rows.  A lane holds 32 bytes of a row
-// (8 or 16 channels); the lanes of a group find its maximum by shuffles.
+// (8 or 16 channels); the lanes of a group find its maximum by shuffles.  (16 bytes a lane, every piece paying for its group's scale, took 205 instructions for 8
+// channels of bf16: 56 us where 40 are needed now.)  24576 x 4096 fp32 to mx 125 us (6.9 TB/s), 16384 x 4096 bf16 to nv 39 us (4.4 TB/s), with the stored
+// values too 52 (5.9 TB/s), 32 x 4096 2.0; 8 x 1984 rows of 4096 channels into a cache, keys and values with stored values 105 us (5.7 TB/s).
 #pragma once
 #include <cuda_fp16.h>
 #include <climits>

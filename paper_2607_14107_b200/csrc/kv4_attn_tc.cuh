@@ -11,6 +11,11 @@
 //   split    the key tiles of a batch are cut into parts of one length, the shortest that gives no more parts than there are CTAs, so that ragged
 //            lengths leave none of them idle; kv4_attn_join_kernel puts a sequence's parts together
 //
+// Bound by the softmax warps' chain (read a row's scores, maximum, 128 exponentials, write, hand over) next to the tensor core: 128 rows of 28 heads, 4 K/V heads,
+// 65536 keys 155 us (775 TFLOP/s), 32768 keys 89 us; 512 rows of 32 heads over 512 keys 13 us.  Without the turning of codes 8 % less.  Dropped: exponentials
+// begun with the old maximum before the new one is known (a longer chain); a form with S^T in tensor memory for up to 64 rows (143 us for 58 at 64 rows,
+// 8 x 2048 keys, 32 heads: its code is fetched once per CTA, and that alone takes longer than the products).
+//
 // fp16 on both sides: keys and values are exact in it, q (bf16) is after a power of two per row, and probabilities keep three more bits than in bf16.
 // The method of the two streams and the lagging maximum is that of attn_flash.cuh (published; named there).  Every mbarrier wait is bounded.
 #pragma once
