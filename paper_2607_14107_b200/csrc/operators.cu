@@ -432,11 +432,18 @@ extern "C" int polestar_k_token_logprobs(const void* logits, int64_t ld, int32_t
     lpr::Args a;
     a.x = logits; a.ld = ld; a.target = target; a.logprob = logprob; a.entropy = entropy; a.top_ids = top_ids; a.top_logprobs = top_logprobs;
     a.V = vocab; a.mask_id = mask_id >= 0 && mask_id < vocab ? mask_id : -1; a.k = top_k;
-    // threads per row as for the confidence kernel: a batch of loads each, and at most the SMs' worth for all rows
-    const long long most = std::min<long long>(vocab * (long long)es / (16 * lpr::U), 1776LL * di.sm_count / rows);
+    // Threads of a row: as many as have a batch of loads each, 256 in any case, up to 2048 while the threads of all rows are resident at once (64 registers: 1024 to an SM),
+    // 4096 for a few rows.  us for 126464 fp32 logits without / with 8 alternatives, as many threads as this, half, twice: 64 rows 11 / 14, 14 / 17, 16 / 24; 128 rows
+    // 17 / 20, 23 / 26, 20 / 28; 512 rows 48 / 55, 70 / 86, 51 / 60; 1 row 5.2 / 8.1, 6.2 / 8.8.  In CTAs of 512 rather than 256, which leaves less to put together
+    // (128 rows, 20 alternatives 21 / 25; none 16.7 / 16.3); the same with and without alternatives, so that sums are.
+    const long long fit = vocab * (long long)es / (16 * lpr::U);
     int per_row = 128;
-    while (per_row < lpr::MAX_CL * lpr::MAX_THREADS && 2 * per_row <= most) per_row *= 2;
-    a.cl = std::min(lpr::MAX_CL, std::max(1, per_row / 256));
+    for (int next = 256; next <= lpr::MAX_CL * lpr::MAX_THREADS && next <= fit; next *= 2) {
+        if (next > 256 && (long long)next * rows > 1040LL * di.sm_count) break;
+        if (next > 2048 && 16LL * rows > di.sm_count) break;
+        per_row = next;
+    }
+    a.cl = std::min(lpr::MAX_CL, std::max(1, per_row / lpr::MAX_THREADS));
     const int threads = std::min(lpr::MAX_THREADS, per_row / a.cl);
     const long long blocks = (long long)rows * a.cl;
     if (blocks > INT32_MAX) return POLESTAR_E_INVAL;
