@@ -255,18 +255,18 @@ gemm_stream_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
 // whole blocks; every CTA needs those of its own rows of A and of all 256 rows of B.  Persistent: pairs take the tiles in an order in which those in
 // flight share their operands.  There is one accumulator (two of 256 columns would leave no tensor memory for scales): eight warps drain it into
 // registers, 128 columns each, and hand it back before they store.  A lane has a row, so its stores would touch 32 lines per instruction (8192 cycles of
-// the load/store unit for a tile of fp32, more than its products take); rows of 128 bytes go through two swizzled boxes per warp and leave as tensor
+// the load/store unit for a tile of fp32, more than its products take); rows of 128 bytes go through a swizzled box per warp and leave as tensor
 // stores.  Those write whole 16 bytes, also behind the last column: where a row's end or its stride is no multiple of that, the warp stores the boxes'
 // rows element by element.
-// 16384 x 4096 x 4096, bf16 out 127 us (4.3 PFLOP/s), 4096 x 12288 x 4096 102 us (4.0), 997 x 37888 x 3584 fp32 out mx 85 us (3.2).  The tensor pipe is
-// busy 56 % of the time; L2 hands the SMs 9.8 TB/s, which is what a tile of this size asks for at that rate.  Without stores 361 us, without waiting for the
-// accumulator either 334.
+// 8192 x 24576 x 4096, bf16 out 357 us (4.6 PFLOP/s), 4096 x 12288 x 4096 97 us (4.3), 997 x 37888 x 3584 fp32 out mx 72 us (3.8), 512 x 126464 x 4096 131.  L2 hands
+// the SMs 10 TB/s or so, which is what tiles of this size ask for at that rate, and the tensor pipe waits for them: a fifth ring slot in the place of the second
+// output boxes took 79 to 72 us at 997 rows and 137 to 131 at 512.  With four slots, leaving out the stores took 408 to 361, waiting for the accumulator too 334.
 constexpr int PR_THREADS = 384;                  // warp 0: TMA, warp 1: MMA + tensor memory, warps 4..11: epilogue
 constexpr int PR_TILE = 256;
-constexpr int PR_STAGES = 4;
-constexpr uint32_t PR_BOX = 32 * 128;            // a box of outputs: 32 rows of 128 bytes, two of them per epilogue warp
+constexpr int PR_STAGES = 5;
+constexpr uint32_t PR_BOX = 32 * 128;            // a box of outputs, one per epilogue warp: 32 rows of 128 bytes
 __host__ __device__ constexpr uint32_t pr_stage_bytes(int fmt) { return 2 * 128 * 128 + 3 * scale_blocks(fmt) * BLOCK_BYTES; }
-__host__ __device__ constexpr size_t pr_smem_bytes(int fmt) { return 1024 + (size_t)PR_STAGES * ((pr_stage_bytes(fmt) + 1023) / 1024 * 1024) + 8 * 2 * PR_BOX; }
+__host__ __device__ constexpr size_t pr_smem_bytes(int fmt) { return 1024 + (size_t)PR_STAGES * ((pr_stage_bytes(fmt) + 1023) / 1024 * 1024) + 8 * PR_BOX; }
 static_assert(pr_smem_bytes(NV) <= 227 * 1024, "shared memory");
 
 __device__ __forceinline__ void pack16(uint32_t (&w)[4], const float (&f)[4]) {
@@ -294,12 +294,12 @@ __device__ __forceinline__ void umma_fp4_pair(uint32_t d, uint64_t a, uint64_t b
                      " tcgen05.mma.cta_group::2.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n}\n"
                      ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(sa), "r"(sb), "r"(accumulate) : "memory");
 }
-// Tile number -> (row tile, column tile): chunks of 8 row tiles, inside which the row tile runs fastest, so that the pairs at work at one time cover a
-// compact block of the output.
+// Tile number -> (row tile, column tile): chunks of 16 row tiles, inside which the row tile runs fastest, so that the pairs at work at one time cover a
+// compact block of the output (8192 x 24576 x 4096: chunks of 4, 8, 16 385, 364, 357 us).
 __device__ __forceinline__ void pair_tile(int id, int tiles_m, int tiles_n, int& tm, int& tn) {
-    const int per = 8 * tiles_n, chunk = id / per, local = id - chunk * per, rows = min(8, tiles_m - chunk * 8);
+    const int per = 16 * tiles_n, chunk = id / per, local = id - chunk * per, rows = min(16, tiles_m - chunk * 16);
     tn = local / rows;
-    tm = chunk * 8 + (local - tn * rows);
+    tm = chunk * 16 + (local - tn * rows);
 }
 
 template <int FMT, typename OUT>
@@ -405,7 +405,7 @@ gemm_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
         const int quarter = warp & 3, half = (warp - 4) >> 2;
         const uint32_t taddr = tmem + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(half * 128);
         constexpr int PER = 128 / sizeof(OUT), BOXES = 128 / PER;        // columns of a box, boxes of this warp's 128 columns
-        const uint32_t box0 = smem_base + PR_STAGES * STAGE + (uint32_t)(warp - 4) * (2 * PR_BOX);
+        const uint32_t box0 = smem_base + PR_STAGES * STAGE + (uint32_t)(warp - 4) * PR_BOX;
         bool ok = true;
         int n = 0;
         for (int id = pair; id < tiles; id += pairs, ++n) {
@@ -428,8 +428,8 @@ gemm_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
 #pragma unroll
                 for (int x = 0; x < BOXES; ++x) {
                     if (m0 >= g.M || n0 + x * PER >= g.N) break;             // (the same for all lanes)
-                    const uint32_t box = box0 + (uint32_t)(x & 1) * PR_BOX;
-                    if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");      // the store before the last has read its box
+                    const uint32_t box = box0;
+                    if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");      // the store before has read the box
                     __syncwarp();
 #pragma unroll
                     for (int c = 0; c < 8; ++c) {                            // sixteen bytes of the lane's row
