@@ -294,6 +294,9 @@ static int kv4_slots(long long batch, long long wanted) {
 static int kv4_parts(int batch, int slots) {         // of one sequence, at most
     return batch > kv4::MAX_BATCH ? slots / batch : std::min(kv4::MAX_SPLIT, slots - batch + 1);
 }
+// What joining rows of c parts takes: a CTA a row, 520 bytes a part written and read.  (us, 128-wide heads: 2048 rows of 4 parts 7, 8192 rows of 2 and 4 parts 12 and 17, 16384
+// rows of 4 parts 39.)
+static double kv4_join_us(double rows_total, double c) { return 3.0 + rows_total * (c * 1040 / 3e6 + 1.5 / (16 * 148)); }
 // The warp-level kernel: tiles of 8 or 16 rows, four CTAs for every SM, no part of a full sequence shorter than 512 keys, and none at all up to 1024 (joining
 // takes what it gains).
 struct Kv4Warp { int tiles, rows, slots; };
@@ -303,12 +306,13 @@ static Kv4Warp kv4_warp_plan(long long batch, long long R, int cap, int n_heads,
     p.rows = vrows <= 8 ? 8 : 16;
     p.tiles = (int)((vrows + p.rows - 1) / p.rows);
     p.slots = kv4_slots(batch, std::min(4 * 148LL / std::max<long long>(1, (long long)n_kv * p.tiles), cap <= 1024 ? batch : batch * ((cap + 511) / 512)));
+    if (p.slots < 2 * batch) p.slots = (int)batch;        // (a few slots more than sequences are not worth joining for)
     return p;
 }
 // The tensor-core kernel, one CTA per SM: row tiles of 128, one per CTA with its keys split between the streams, or two per CTA.  Two share the turning of
-// codes (a pair takes 2.5 us for 128 keys, one tile 2.1, one of up to 64 rows 1.4), one gives more CTAs where there are few.  Whichever needs less time, by those figures and
-// 8.5 us of start and end, with the keys cut into the number of parts that does (3 us more for joining them); a part of a sequence that fills the cache is
-// no shorter than four key tiles.
+// codes (a pair takes 2.5 us for 128 keys, one tile 2.1, one of up to 64 rows 1.4), one gives more CTAs where there are few.  Whichever needs less time, by those figures, 6 us for
+// the start and end of a CTA, which nothing hides on its SM, 2.5 us for the launch and what joining parts takes; a part of a sequence that fills the cache is no shorter than
+// four key tiles.  (us, parts of 16, 8, 4 key tiles, 64 rows, 2048 keys, 32 heads: 4 sequences 30, 49, 66; 8 sequences 60, 98, 123; 1 sequence 31, -, 19.)
 struct Kv4Tc { int tiles, key_split, slots; double us; };
 static Kv4Tc kv4_tc_plan(long long batch, long long R, int cap, int n_heads, int n_kv) {
     const long long vrows = R * (n_heads / n_kv), row_tiles = (vrows + kv4::TC_ROWS - 1) / kv4::TC_ROWS, key_tiles = (cap + kv4::TC_KEYS - 1) / kv4::TC_KEYS;
@@ -322,7 +326,7 @@ static Kv4Tc kv4_tc_plan(long long batch, long long R, int cap, int n_heads, int
             const int slots = w ? kv4_slots(batch, std::min(148LL * w / per, batch * key_tiles / 4)) : (int)batch;
             const long long c = slots / batch;
             if (w && c < 2) continue;
-            const double us = (w ? (double)w : (double)((per * batch + 147) / 148)) * (double)((key_tiles + c - 1) / c) * tile_us + 8.5 + (w ? 3.0 : 0.0);
+            const double us = (double)((per * slots + 147) / 148) * ((double)((key_tiles + c - 1) / c) * tile_us + 6.0) + 2.5 + (c > 1 ? kv4_join_us((double)batch * R * n_heads, (double)c) : 0.0);
             if (us >= 0.97 * p.us) continue;
             p.us = us; p.key_split = one; p.tiles = (int)tiles; p.slots = slots;
         }
@@ -330,12 +334,11 @@ static Kv4Tc kv4_tc_plan(long long batch, long long R, int cap, int n_heads, int
     return p;
 }
 // Which kernel: the warp-level one turns codes again for every 16 rows, the tensor-core one once for 128 or 256, but it starts slowly and its rows fill whole
-// tiles.  The warp-level one's time as measured: 0.75 us for 16 rows x 128 keys on an SM, or, three CTAs per SM at a time, 1.4 us of latency for 128 keys of a
-// part while the CTAs have an SM for two of theirs, 3.2 us once they share them (2.4 in long parts), and 5 us (3 more for joining parts).  us, warp-level / tensor-core:
-// 7 rows a K/V head, eight ragged sequences of up to 32768 keys 39 / 71; 32 rows, 512 keys x 32 heads 10.5 / 12.8, 8 x 4096 keys x 32 heads 89 / 99; 48 rows,
-// 2 x 1500 keys x 32 heads 30 / 21; 64 rows, 8 x 2048 keys x 32 heads 84 / 58; 224 rows, 300 keys x 4 heads 8.4 / 13.4; 448 rows, 8 x 800 keys x 4
-// heads 40 / 19; 896 rows, 65536 keys x 4 heads 650 / 156.
-static bool kv4_use_tc(int dtype, int head_dim, const Kv4Warp& w, const Kv4Tc& t, long long batch, int cap, int n_kv) {
+// tiles.  The warp-level one's time as measured: 1.0 us for 16 rows x 128 keys on an SM, or, three CTAs per SM at a time, 1.4 us of latency for 128 keys of a
+// part while the CTAs have an SM for two of theirs, 3.2 us once they share them (2.4 in long parts), all of it times 0.75 for 8 rows, and 5 us and the joining.  us, warp-level / tensor-core:
+// 7 rows a K/V head, eight ragged sequences of up to 32768 keys 36 / 112; 32 heads, 32 rows, 512 keys 12.9 / 12.7, 8 x 2048 keys 78 / 59; 64 rows, 2048 keys 33 / 19, 8 x 2048
+// 121 / 60; 63 rows x 4 heads, 2048 keys 14.5 / 17.3, 8 x 2048 32 / 20; 896 rows, 65536 keys x 4 heads 814 / 155.
+static bool kv4_use_tc(int dtype, int head_dim, const Kv4Warp& w, const Kv4Tc& t, long long batch, long long R, int cap, int n_heads, int n_kv) {
     if (dtype != POLESTAR_BF16 || head_dim != kv4::TC_DH) return false;
     const int forced = read_switch(g_kv4_kernel);
     if (forced) return forced == 2;
@@ -343,7 +346,8 @@ static bool kv4_use_tc(int dtype, int head_dim, const Kv4Warp& w, const Kv4Tc& t
     const double all = (double)batch * n_kv * w.tiles * ((cap + 127) / 128);
     double tile = 1.4 + 1.8 * std::min(1.0, std::max(0.0, (ctas - 74) / 100));
     if (part >= 8) tile = std::min(tile, 2.4);
-    return t.us < std::max(all / 148 * 0.75, std::max(1.0, ctas / 444) * part * tile) + 5 + (w.slots > batch ? 3 : 0);
+    const double join = w.slots > batch ? kv4_join_us((double)batch * R * n_heads, (double)w.slots / batch) : 0.0;
+    return t.us < (w.rows == 8 ? 0.75 : 1.0) * std::max(all / 148, std::max(1.0, ctas / 444) * part * tile) + 5 + join;
 }
 static bool kv4_attention_shape_ok(int batch, int R, int cap, int n_heads, int n_kv, int head_dim) {
     return kv4_shape_ok(batch, R, cap, n_kv, head_dim) && R <= 65536 && n_heads > 0 && n_heads <= 1024 && n_heads % n_kv == 0;
@@ -400,7 +404,7 @@ extern "C" int polestar_k_kv4_attention(const void* q, const uint8_t* kc, const 
     a.batch = batch; a.R = R; a.cap = cap; a.n_heads = n_heads; a.n_kv = n_kv; a.rows_total = (long long)batch * R * n_heads;
     const Kv4Tc plan = kv4_tc_plan(batch, R, cap, n_heads, n_kv);
     const Kv4Warp wplan = kv4_warp_plan(batch, R, cap, n_heads, n_kv);
-    const bool tc = kv4_use_tc(dtype, head_dim, wplan, plan, batch, cap, n_kv);
+    const bool tc = kv4_use_tc(dtype, head_dim, wplan, plan, batch, R, cap, n_heads, n_kv);
     a.slots = tc ? plan.slots : wplan.slots;
     const int parts = kv4_parts(batch, a.slots);
     a.part_n = parts > 1 ? (int*)scratch : nullptr;
