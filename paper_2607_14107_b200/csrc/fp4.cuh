@@ -36,7 +36,8 @@ __device__ __forceinline__ size_t tiled_offset(long long r, int g, int g4) {
 }
 
 // Correctly rounded quotients by a divisor b with r = RN(1 / b): q = x r is within an ulp, and one step q + (x - b q) r rounds correctly (Markstein,
-// 1990) while nothing overflows or underflows: |b| and |x| within 2^-100 .. 2^100 (x = 0 too).
+// 1990) while nothing overflows or underflows: |b| and |x| within 2^-100 .. 2^100 (x = 0 too) and the quotient below that, since an infinite q makes NaN of
+// the correction.  (A quotient that underflows is a little off, which no scale sees: those below 2^-124 are all one byte.)
 __device__ __forceinline__ float divide(float x, float b, float r) {
     const float q = x * r;
     return fmaf(fmaf(-b, q, x), r, q);
@@ -46,21 +47,21 @@ __device__ __forceinline__ bool in_range(float x) { return x >= FAST_LO && x <= 
 // the tensor's factor and what follows from it alone
 struct Factor {
     float t, b, r;                               // b: divisor of a group's maximum (6 t or t), r = RN(1 / b)
-    bool fast;
+    float hi;                                    // maxima up to here have ordinary quotients (-1: none, b is out of range)
 };
 template <int FMT> __device__ __forceinline__ Factor make_factor(const float* p) {
     Factor f;
     f.t = p ? __ldg(p) : 1.f;
     f.b = FMT == NV ? __fmul_rn(f.t, 6.f) : f.t;
     f.r = __frcp_rn(f.b);
-    f.fast = in_range(f.b);
+    f.hi = in_range(f.b) ? fminf(FAST_HI, f.b * FAST_HI) : -1.f;
     return f;
 }
 // scale of a group from the largest magnitude's bits (an integer maximum: NaN and infinity stay on top)
 template <int FMT>
 __device__ __forceinline__ float group_scale(uint32_t amax, const Factor& f, uint32_t* byte) {
     const float a = __uint_as_float(amax);
-    float q = f.fast && in_range(a) ? divide(a, f.b, f.r) : __fdiv_rn(a, f.b);
+    float q = a >= FAST_LO && a <= f.hi ? divide(a, f.b, f.r) : __fdiv_rn(a, f.b);
     if (FMT == NV) {
         if (amax >= 0x7f800000u) q = __uint_as_float(0x7fc00000u);
         uint16_t e;
