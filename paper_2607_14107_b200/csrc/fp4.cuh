@@ -115,8 +115,10 @@ template <> struct Vec<__nv_bfloat16> {
 
 // One lane's piece of a row: 32 bytes of it, a group's worth or less, so that what a group costs once (its maximum, scale and reciprocal) is paid by as few
 // lanes as may be.  All lanes of the warp take part; the lanes of a group are neighbours.  Results: the codes, four bits each, channel 0 lowest, the group's
-// scale byte, and the stored values in the row's type.  The conversion to E2M1 rounds to nearest, ties to the even code, and saturates; groups whose
-// unit s t is so far out that the division's steps could overflow or underflow divide by the instruction.
+// scale byte, and the stored values in the row's type.  The conversion to E2M1 rounds to nearest, ties to the even code, and saturates.  Groups whose unit
+// s t is far out divide by the instruction, and so do those whose maximum is far above the factor: s saturates there, and a quotient beyond fp32 would make NaN
+// of the division's last step, which converts to +6 whatever the sign.  (Elsewhere |x| is below 9 s t, the least s of nv being half the wanted one at worst; an |x| so
+// small that the steps underflow is below half a code.)
 template <typename T> struct Piece {
     static constexpr int N = 2 * Vec<T>::N, WORDS = N / 8;                 // channels, words of codes
     uint4 w[2];
@@ -136,7 +138,7 @@ __device__ __forceinline__ void encode(const Piece<T>& x, const Factor& f, uint3
     Vec<T>::unpack(x.w[1], v + H);
 #pragma unroll
     for (int h = 0; h < Piece<T>::WORDS; ++h) codes[h] = 0u;
-    if (__builtin_expect(in_range(u), 1)) {
+    if (__builtin_expect(in_range(u) && __uint_as_float(am) <= f.hi, 1)) {
         const float r = __frcp_rn(u);
         const uint64_t r2 = f2_pack(r, r), nu = f2_pack(-u, -u);
 #pragma unroll
