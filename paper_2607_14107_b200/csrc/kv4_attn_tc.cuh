@@ -312,7 +312,10 @@ __global__ void __launch_bounds__(TC_THREADS, 1) kv4_attn_tc_kernel(const __grid
         __syncwarp();
         if (lane == 0) mbar_arrive(bar_q);
         asm volatile("bar.sync 1, 256;" ::: "memory");             // the rows' units
-        const float unit = (float)((double)unit_sh[ksplit ? 0 : g][row] * (a.scale * (double)(a.tk ? __ldg(a.tk) : 1.f)));
+        // (a unit of 0, of a row of zeros and a small factor, would make NaN of the -inf of keys that are not there; at the smallest normal one, scores are still
+        // nothing: below 2^-100)
+        float unit = (float)((double)unit_sh[ksplit ? 0 : g][row] * (a.scale * (double)(a.tk ? __ldg(a.tk) : 1.f)));
+        if (fabsf(unit) < 1.17549435e-38f) unit = 1.17549435e-38f;
         const float tv = a.tv ? __ldg(a.tv) : 1.f;
 
         float m = -INFINITY, l = 0.f;
@@ -343,7 +346,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) kv4_attn_tc_kernel(const __grid
 #pragma unroll
                 for (int c = 0; c < 4; ++c) tm4[c] = fmaxf(tm4[c], __uint_as_float(sc[c][i]));
             float tm = fmaxf(fmaxf(tm4[0], tm4[1]), fmaxf(tm4[2], tm4[3]));
-            tm = tm == -INFINITY ? tm : tm * unit;                 // (unit >= 0: the maximum commutes with it; a unit of 0 makes all scores 0)
+            tm *= unit;                                            // (unit > 0: the maximum commutes with it)
             if (k == 0) {
                 m = tm;
             } else if (__builtin_expect(__any_sync(0xffffffffu, tm > m + SLACK), 0)) {

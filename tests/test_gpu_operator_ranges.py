@@ -6,6 +6,7 @@ import torch
 import fp4_reference as F
 from paper_2607_14107_b200 import binding as Bd
 from test_gpu_fp4 import check_rows, f32
+from test_gpu_kv4 import reference, run
 
 pytestmark = pytest.mark.gpu
 
@@ -65,3 +66,46 @@ def test_appended_rows_beyond_fp32(t, dtype):
     for x, c, s in ((k, kc, ks), (v, vc, vs)):
         want_c, want_s, _ = F.quantize(f32(x).reshape(b, R, nkv, dh), F.NV, t)
         assert np.array_equal(c.cpu().numpy(), F.pack(want_c)) and np.array_equal(s.cpu().numpy(), want_s)
+
+
+def cache_of(k, v, tk, tv):
+    """Rows [b, cap, n_kv, dh] -> a 4-bit cache and the values that it stands for."""
+    got = []
+    for x, t in ((k, tk), (v, tv)):
+        c, s, _ = F.quantize(x.numpy(), F.NV, t)
+        got.append((torch.from_numpy(F.pack(c)).cuda(), torch.from_numpy(s).cuda(), torch.from_numpy(F.values(c, s, F.NV, t))))
+    return got
+
+
+def force(monkeypatch, kernel):
+    monkeypatch.setenv("POLESTAR_KV4_KERNEL", str(kernel))
+    Bd.polestar_reload_env()
+
+
+@pytest.mark.parametrize("kernel,dtype,dh", [(1, "bf16", 128), (2, "bf16", 128), (0, "f32", 128), (0, "bf16", 64)])
+@pytest.mark.parametrize("tk", [1.0, 4e-7, 1e-7, 2.0 ** -126])
+@pytest.mark.parametrize("R,cap,lens", [(5, 300, [300, 129, 128]), (300, 257, [257, 1, 100]), (3, 4200, [4199, 4096, 130])])
+def test_zero_rows_are_the_mean_of_the_values(monkeypatch, kernel, dtype, dh, tk, R, cap, lens):
+    # a row of zeros (padding) weighs every key alike, whatever the keys' factor and wherever the length ends in a tile
+    force(monkeypatch, kernel)
+    b, nh, nkv, tv = 3, 4, 2, 0.005
+    g = torch.Generator().manual_seed(5)
+    k, v = torch.randn((b, cap, nkv, dh), generator=g) * tk * 50, torch.randn((b, cap, nkv, dh), generator=g)
+    (kc, ks, k64), (vc, vs, v64) = cache_of(k, v, tk, tv)
+    q = torch.randn((b, R, nh, dh), generator=g)
+    q[:, ::2] = 0.0
+    if tk < 1:
+        q[:, 1] = 1e-38                                            # its scores are as good as 0
+    out, lse = run(q.flatten(2).to(DT[dtype]).cuda(), kc, ks, vc, vs, tk, tv, lens)
+    want, want_lse, size = reference(q.to(DT[dtype]).double(), k64, v64, lens, nh)
+    got, got_lse = out.double().cpu().view_as(want), lse.double().cpu()
+    rows = torch.zeros(R, dtype=torch.bool)
+    rows[::2] = True
+    if tk < 1:
+        rows[1] = True
+    # probabilities are 2^7 or, at factors of 2^-126, off by less than 2^-100: exact in fp16.  Sums of up to `cap` values of 128 |v| add 2^-23 (truncated)
+    # per addition of 16 keys; then the factor, the quotient and the output's rounding
+    tol = size * 2.0 ** -23 * (cap / 16 + 16) + want.abs() * (2.0 ** -22 + torch.finfo(DT[dtype]).eps / 2)
+    assert ((got - want).abs() <= tol)[:, rows].all(), ((got - want).abs() / tol)[:, rows].max().item()
+    assert ((got_lse - want_lse).abs() <= 2.0 ** -22 * want_lse.abs() + 2.0 ** -20)[:, rows].all()
+    assert torch.isfinite(got).all() and torch.isfinite(got_lse).all()
