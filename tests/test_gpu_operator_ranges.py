@@ -109,3 +109,40 @@ def test_zero_rows_are_the_mean_of_the_values(monkeypatch, kernel, dtype, dh, tk
     assert ((got - want).abs() <= tol)[:, rows].all(), ((got - want).abs() / tol)[:, rows].max().item()
     assert ((got_lse - want_lse).abs() <= 2.0 ** -22 * want_lse.abs() + 2.0 ** -20)[:, rows].all()
     assert torch.isfinite(got).all() and torch.isfinite(got_lse).all()
+
+
+@pytest.mark.parametrize("kernel", [1, 2])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("fmt", [F.NV, F.MX])
+@pytest.mark.parametrize("M,N,K", [(5, 131, 64), (70, 256, 2048), (300, 520, 192)])
+@pytest.mark.parametrize("ta,tb,shrink", [(1e-22, 3e-22, 1.0), (1e-30, 1e-14, 1.0), (1e25, 1e14, 1e-4), (2.0 ** 100, 2.0 ** 30, 1e-4), (2.0 ** -126, 2.0 ** -100, 1.0),
+                                          (2.0 ** 127, 2.0 ** 126, 1e-4), (3e-20, 1e-19, 1.0), (0.013, 3e5, 1.0)])
+def test_far_factors_of_a_product(monkeypatch, kernel, M, N, K, fmt, dtype, ta, tb, shrink):
+    # the two factors' product may lie outside fp32 although the result does not, and a row of zeros stays one
+    monkeypatch.setenv("POLESTAR_FP4_KERNEL", str(kernel))
+    Bd.polestar_reload_env()
+    g = torch.Generator().manual_seed(M)
+    x = torch.randn((M, K), generator=g) * shrink
+    x[M // 2] = 0.0
+    c, s, _ = F.quantize(x.numpy(), fmt, 0.01)
+    av = torch.from_numpy(F.values(c, s, fmt))
+    y = torch.randn((N, K), generator=g) * shrink
+    bc, bs, _ = F.quantize(y.numpy(), fmt, 0.01)
+    bv = torch.from_numpy(F.values(bc, bs, fmt))
+    ta, tb = (torch.tensor([t], dtype=torch.float32, device="cuda") for t in (ta, tb))
+    out = torch.full((M, N), 5.0, dtype=dtype, device="cuda")
+    Bd.polestar_k_fp4_matmul(torch.from_numpy(F.pack(c)).cuda(), torch.from_numpy(F.tile_scales(s)).cuda(), torch.from_numpy(F.pack(bc)).cuda(),
+                             torch.from_numpy(F.tile_scales(bs)).cuda(), out, fmt, ta, tb)
+    factor = ta.double().cpu().item() * tb.double().cpu().item()
+    want, size = av @ bv.T * factor, av.abs() @ bv.abs().T * factor
+    got = out.double().cpu()
+    # as in the tests of the product: 2^-22 of the magnitudes per instruction and part, 2^-24 for each factor and the product with it, the output's rounding; results
+    # below the normal range are rounded to its step
+    tol = size * (2.0 ** -22 * (K / 64 + 8) + 2.0 ** -22) + want.abs() * torch.finfo(dtype).eps / 2 + 2.0 ** -126 * torch.finfo(dtype).eps
+    top = torch.finfo(dtype).max
+    fits = want.abs() + tol < top
+    assert fits.any() or factor > 1e60
+    assert ((got - want).abs() <= tol)[fits].all(), ((got - want).abs() / tol)[fits].max().item()
+    over = want.abs() - tol > 1.01 * top
+    assert (torch.isinf(got) & (torch.sign(got) == torch.sign(want)))[over].all()
+    assert not torch.isnan(got).any() and (got[M // 2] == 0).all()
