@@ -446,7 +446,8 @@ int polestar_k_kv4_append(const void *k_dev, const void *v_dev, const int32_t *i
  *   q_dev [batch][R][n_heads*head_dim], out_dev the same, F32 or BF16; query head h reads K/V head h / (n_heads / n_kv)
  *   lens_dev int32 [batch]: keys of every sequence (NULL: cap; clamped to 0 .. cap); cache rows behind them are not read
  *   lse_dev float [batch][R][n_heads] (natural logarithm; NULL: skipped), to join the rows with attention over other keys
- * A sequence without keys gives zero rows and lse = -inf.  head_dim 64 or 128, n_heads <= 1024.
+ * A sequence without keys gives zero rows and lse = -inf.  A score above fp32's range makes its row and lse NaN; scores below it weigh nothing, and a row that has
+ * no others is NaN.  head_dim 64 or 128, n_heads <= 1024.
  *   scratch_dev: >= polestar_k_kv4_scratch_bytes(...) bytes, of one call at a time.
  * q, out, the cache's four arrays and scratch 16-byte aligned. */
 size_t polestar_k_kv4_scratch_bytes(int32_t batch, int32_t R, int32_t cap, int32_t n_heads, int32_t n_kv, int32_t head_dim);

@@ -3,7 +3,7 @@
 //   s_j = q . k_j / sqrt(head_dim),  j < length of the sequence;   out = sum_j softmax(s)_j v_j,   lse = log sum_j e^(s_j)
 //
 // What a code and its scale stand for has six significant bits, so every key and value is exact in fp16 (and bf16); the tensors' factors are
-// applied to the scores and to the finished rows.  A row without keys is zero, its lse -inf.
+// applied to the scores and to the finished rows.  A row without keys is zero, its lse -inf; one whose scores are all below fp32's range is NaN.
 //
 // kv4_attn_warp_kernel (mma.sync m16n8k16, any type, head_dim 64 or 128): for few rows, where the stream of the cache and the instructions that
 // unpack it are the bound.  Sixteen keys are the 16 rows of the first operand (S^T = K Q^T) and sixteen channels of values are (O^T = V^T P^T), so
@@ -446,6 +446,7 @@ __global__ void __launch_bounds__(THREADS) kv4_attn_warp_kernel(const __grid_con
             *reinterpret_cast<float4*>(a.part_o + p * DH + c) = acc;
             if (c == 0) a.part_ml[p] = make_float2(mm, ll);
         } else {
+            if (ll == 0.f && hi > 0) ll = __uint_as_float(0x7fc00000u);       // (keys, but every score -inf; lo is 0 here)
             const float inv = ll == 0.f ? 0.f : tv / ll;
             T* out = (T*)a.out + row * DH + c;
             store_pair<T>(out, acc.x * inv, acc.y * inv);
@@ -465,7 +466,7 @@ __global__ void __launch_bounds__(JOIN_THREADS) kv4_attn_join_kernel(const __gri
     __shared__ float red[2][JW];
     const int t = threadIdx.x, lane = t & 31, warp = t >> 5;
     const size_t row = blockIdx.x;
-    const int parts = __ldcg(a.part_n + row / ((size_t)a.R * a.n_heads));
+    const int seq = (int)(row / ((size_t)a.R * a.n_heads)), parts = __ldcg(a.part_n + seq);
     float2 ml = make_float2(-INFINITY, 0.f);
     static_assert(MAX_SPLIT <= JOIN_THREADS, "a part per thread");
     if (t < parts) ml = __ldcg(a.part_ml + (size_t)t * a.rows_total + row);
@@ -483,6 +484,7 @@ __global__ void __launch_bounds__(JOIN_THREADS) kv4_attn_join_kernel(const __gri
     float ll = red[1][0];
 #pragma unroll
     for (int i = 1; i < JW; ++i) ll += red[1][i];
+    if (ll == 0.f && seq_len(a, seq) > 0) ll = __uint_as_float(0x7fc00000u);             // (keys, but every score -inf)
     float acc[PER];
 #pragma unroll
     for (int c = 0; c < PER; ++c) acc[c] = 0.f;

@@ -404,6 +404,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) kv4_attn_tc_kernel(const __grid
             w0 = m0 == -INFINITY ? 1.f : ex2(m0 - m); w1 = m1 == -INFINITY ? 1.f : ex2(m1 - m);       // (nothing but NaN scores: m = -inf, l = NaN)
             l = l0 * w0 + l1 * w1;
         }
+        if (l == 0.f && n > 0 && !a.part_n) l = __uint_as_float(0x7fc00000u);       // (keys, but every score -inf)
         const bool none = l == 0.f;                        // no keys: the accumulators hold nothing
         if ((cnt > 0 || ksplit || n == 0) && vr < vrows) {
             const size_t ro = q_row(vr);

@@ -1,4 +1,6 @@
 """The 4-bit operators at the ends of what their arguments may be: factors, rows and scores far from what models hold."""
+import math
+
 import numpy as np
 import pytest
 import torch
@@ -146,3 +148,40 @@ def test_far_factors_of_a_product(monkeypatch, kernel, M, N, K, fmt, dtype, ta, 
     over = want.abs() - tol > 1.01 * top
     assert (torch.isinf(got) & (torch.sign(got) == torch.sign(want)))[over].all()
     assert not torch.isnan(got).any() and (got[M // 2] == 0).all()
+
+
+@pytest.mark.parametrize("kernel,dtype,dh", [(1, "bf16", 128), (2, "bf16", 128), (0, "f32", 128), (0, "bf16", 64)])
+@pytest.mark.parametrize("cap,lens", [(1, [1, 0]), (200, [200, 130]), (5000, [5000, 64])])
+def test_scores_beyond_fp32(monkeypatch, kernel, dtype, dh, cap, lens):
+    # -inf weighs nothing beside other scores; rows whose scores are all -inf have no softmax: NaN, and not the zero row of a sequence without keys
+    force(monkeypatch, kernel)
+    b, R, nh, tk, tv = 2, 4, 2, 1e7, 0.01
+    g = torch.Generator().manual_seed(6)
+    k, v = torch.rand((b, cap, 1, dh), generator=g) * 1e10 + 1e9, torch.randn((b, cap, 1, dh), generator=g)
+    k[:, 1::2] = 0.0                                                # every second key scores 0
+    (kc, ks, k64), (vc, vs, v64) = cache_of(k, v, tk, tv)
+    q = torch.full((b, R, nh, dh), -1e30)
+    q[:, 1] = 1e-12
+    q = q.to(DT[dtype])
+    out, lse = run(q.flatten(2).cuda(), kc, ks, vc, vs, tk, tv, lens)
+    want, want_lse, size = reference(q.double(), k64, v64, lens, nh)
+    got, got_lse = out.double().cpu().view_as(want), lse.double().cpu()
+    for i, n in enumerate(lens):
+        for r in (0, 2, 3):
+            if n == 0:
+                assert not got[i, r].any() and (got_lse[i, r] == -math.inf).all()
+            elif n == 1:
+                assert torch.isnan(got[i, r]).all() and torch.isnan(got_lse[i, r]).all()
+            else:
+                tol = size * (2.0 ** -23 * (cap / 16 + 16)) + want.abs() * (2.0 ** -22 + torch.finfo(DT[dtype]).eps / 2)
+                assert ((got - want).abs() <= tol)[i, r].all()
+                assert ((got_lse - want_lse).abs() <= 1e-5)[i, r].all()
+    # all keys: every one of them far below
+    k[:, 1::2] = k[:, :1]
+    (kc, ks, k64), _ = cache_of(k, v, tk, tv)
+    out, lse = run(q.flatten(2).cuda(), kc, ks, vc, vs, tk, tv, lens)
+    got, got_lse = out.cpu().view_as(want), lse.cpu()
+    for i, n in enumerate(lens):
+        for r in (0, 2, 3):
+            assert torch.isnan(got[i, r]).all() and torch.isnan(got_lse[i, r]).all() if n else not got[i, r].any() and (got_lse[i, r] == -math.inf).all()
+        assert torch.isfinite(got[i, 1]).all()
