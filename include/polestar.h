@@ -442,7 +442,9 @@ int polestar_k_kv4_append(const void *k_dev, const void *v_dev, const int32_t *i
 
 /* Attention of query rows over that cache (Eq. 3 without the drift of stored rows; bidirectional: every row sees every key of its sequence):
  *   s_j = q . k_j / sqrt(head_dim) for j < len,  out = sum_j softmax(s)_j v_j,  lse = log sum_j e^(s_j)
- * with keys and values as the cache stores them (exact; bf16: probabilities rounded to 16 bits, fp32: to 22), fp32 sums.
+ * with keys and values as the cache stores them (exact) and fp32 sums.  bf16: probabilities are held in fp16 (11 bits, no finer than 2^-32 of the row's largest), and
+ * so is q after a power of two for the row (exact, but for entries below 2^-17 of its largest, whose last places go at 2^-25 of it).  fp32: both have
+ * 22 bits, probabilities no finer than 2^-44 of the largest, q than 2^-37.
  *   q_dev [batch][R][n_heads*head_dim], out_dev the same, F32 or BF16; query head h reads K/V head h / (n_heads / n_kv)
  *   lens_dev int32 [batch]: keys of every sequence (NULL: cap; clamped to 0 .. cap); cache rows behind them are not read
  *   lse_dev float [batch][R][n_heads] (natural logarithm; NULL: skipped), to join the rows with attention over other keys

@@ -28,6 +28,7 @@ constexpr int MAX_SPLIT = 128;
 constexpr int JOIN_THREADS = 128;
 constexpr int MAX_BATCH = 32;                    // sequences whose parts are cut to measure (a lane each)
 constexpr float SLACK = 8.f;                     // log2 of how far the running maximum may lag behind
+constexpr float TERM = 4096.f;                   // the second of two fp16 terms is stored times this: at most 2^15 beside a first one of 2^15, and steps down to 2^-36
 constexpr float LIFT = 7.f;                      // probabilities are 2^(s - m + LIFT): fp16 then keeps them down to 2^-31 of the largest
 
 struct Args {
@@ -144,7 +145,8 @@ __device__ __forceinline__ uint32_t transpose8x8(uint32_t a) {
 }
 
 // grid: x = tile of 8 NB rows x part, y = K/V head.  Lane (g = lane / 4, t = lane % 4).
-// fp32 rows: q and the probabilities are each two fp16 terms (22 bits), with a product per term.
+// fp32 rows: q and the probabilities are each two fp16 terms (22 bits), the second times TERM, with a product per term.  (Without that factor what is below
+// 2^-25 is lost: entries of q beside much larger ones, and probabilities below 2^-32 of the largest, 65536 of which weigh 2^-16.)
 template <typename T, int DH, int NB>
 __global__ void __launch_bounds__(THREADS) kv4_attn_warp_kernel(const __grid_constant__ Args a) {
     KERNEL_PROLOGUE(23);   // kv4_attn_warp_kernel
@@ -242,7 +244,7 @@ __global__ void __launch_bounds__(THREADS) kv4_attn_warp_kernel(const __grid_con
                 qf[0][n][s][p] = w;
                 if (TERMS == 2) {
                     const float2 r = unpack_half(w);
-                    qf[TERMS - 1][n][s][p] = pack_half(v.x - r.x, v.y - r.y);
+                    qf[TERMS - 1][n][s][p] = pack_half((v.x - r.x) * TERM, (v.y - r.y) * TERM);
                 }
             }
     }
@@ -311,7 +313,7 @@ __global__ void __launch_bounds__(THREADS) kv4_attn_warp_kernel(const __grid_con
 #pragma unroll
         for (int n = 0; n < NB; ++n)
 #pragma unroll
-            for (int x = 0; x < 4; ++x) s[n][x] = SUMS == 1 ? part_s[0][n][x] : (part_s[0][n][x] + part_s[SUMS / 2][n][x]) + part_s[SUMS - 1][n][x];
+            for (int x = 0; x < 4; ++x) s[n][x] = SUMS == 1 ? part_s[0][n][x] : fmaf(part_s[SUMS - 1][n][x], 1.f / TERM, part_s[0][n][x] + part_s[SUMS / 2][n][x]);
         bool grow = false;
         float y[NB][4];                          // score - m + LIFT
         if (__builtin_expect(j0 + CHUNK > hi, 0)) {
@@ -361,7 +363,7 @@ __global__ void __launch_bounds__(THREADS) kv4_attn_warp_kernel(const __grid_con
                 pf[0][n][y] = transpose8x8(w);   // keys g (+ 8), rows 2t.. -> keys 2t.. (+ 8), row g
                 if (TERMS == 2) {
                     const float2 back = unpack_half(w);
-                    pf[TERMS - 1][n][y] = transpose8x8(pack_half(p[2 * y] - back.x, p[2 * y + 1] - back.y));
+                    pf[TERMS - 1][n][y] = transpose8x8(pack_half((p[2 * y] - back.x) * TERM, (p[2 * y + 1] - back.y) * TERM));
                 }
             }
         }
@@ -398,6 +400,8 @@ __global__ void __launch_bounds__(THREADS) kv4_attn_warp_kernel(const __grid_con
                     } else {                     // (a chunk's sums by themselves, then rounded to nearest)
                         float d[4] = {0.f, 0.f, 0.f, 0.f};
                         mma16816(d, fa, pf[TERMS - 1][n][0], pf[TERMS - 1][n][1]);
+#pragma unroll
+                        for (int z = 0; z < 4; ++z) d[z] *= 1.f / TERM;
                         mma16816(d, fa, pf[0][n][0], pf[0][n][1]);
 #pragma unroll
                         for (int z = 0; z < 4; ++z) o[4 * w + x][n][z] += d[z];

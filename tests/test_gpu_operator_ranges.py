@@ -185,3 +185,52 @@ def test_scores_beyond_fp32(monkeypatch, kernel, dtype, dh, cap, lens):
         for r in (0, 2, 3):
             assert torch.isnan(got[i, r]).all() and torch.isnan(got_lse[i, r]).all() if n else not got[i, r].any() and (got_lse[i, r] == -math.inf).all()
         assert torch.isfinite(got[i, 1]).all()
+
+
+@pytest.mark.parametrize("dh", [64, 128])
+@pytest.mark.parametrize("R,cap", [(1, 3000), (20, 700)])
+def test_fp32_rows_of_wide_range(dh, R, cap):
+    # one large entry that meets keys of zero: the scores are those of the small entries, which have to keep their places
+    g = torch.Generator().manual_seed(9)
+    k, v = torch.randn((1, cap, 1, dh), generator=g) * 3e5, torch.randn((1, cap, 1, dh), generator=g)
+    k[..., :16] = 0.0
+    (kc, ks, k64), (vc, vs, v64) = cache_of(k, v, 200.0, 0.005)
+    q = torch.randn((1, R, 2, dh), generator=g) * 1e-6
+    q[..., 3] = 1.5
+    out, lse = run(q.flatten(2).cuda(), kc, ks, vc, vs, 200.0, 0.005, None)
+    want, want_lse, size = reference(q.double(), k64, v64, [cap], 2)
+    # q is held to 2^-22 of an entry, or 2^-37 of twice the row's largest; then sums of dh terms in fp32, one rounding each for unit and score
+    qk = torch.stack([q[0, :, h].double().abs() @ k64[0, :, 0].abs().T for h in range(2)], 1).amax(-1)[None] / math.sqrt(dh)
+    s_err = qk * 2.0 ** -21 + 3.0 * 2.0 ** -37 * k64[0, :, 0].abs().sum(-1).max() / math.sqrt(dh)
+    rel = 2 * s_err + 2.0 ** -20 + 2.0 ** -24 * (cap / 8 + 64)
+    got = out.double().cpu().view_as(want)
+    tol = (rel + 2.0 ** -22)[..., None] * size + want.abs() * 2.0 ** -24
+    assert ((got - want).abs() <= tol).all(), ((got - want).abs() / tol).max().item()
+    assert ((lse.double().cpu() - want_lse).abs() <= rel + 2.0 ** -22 * want_lse.abs()).all()
+
+
+@pytest.mark.parametrize("dh", [64, 128])
+@pytest.mark.parametrize("R", [1, 12])
+def test_fp32_probabilities_far_below_the_largest(R, dh):
+    # a few keys take nearly all the weight and have the value 0 in half of the channels: what the others add there is the output
+    cap = 20000
+    g = torch.Generator().manual_seed(10)
+    k, v = torch.zeros((1, cap, 1, dh)), torch.rand((1, cap, 1, dh), generator=g) + 0.5
+    k[0, :, 0, 17] = torch.randint(0, 2, (cap,), generator=g).float()          # scores 0 or about 0.1 ...
+    j = torch.arange(cap)
+    top = (j % 16 == 3) & (j // 16 % 8 < 4)
+    k[0, top, 0, 0] = 6.0                                                      # ... and about 23: the others' probabilities are near 2^-33 of the largest
+    v[0, top, 0, dh // 2:] = 0.0
+    (kc, ks, k64), (vc, vs, v64) = cache_of(k, v, 0.01, 0.01)
+    q = torch.zeros((1, R, 2, dh))
+    q[..., 0] = math.log(2) * 34 * math.sqrt(dh) / 6.0
+    q[..., 17] = 0.1 * math.sqrt(dh)
+    out, _ = run(q.flatten(2).cuda(), kc, ks, vc, vs, 0.01, 0.01, None)
+    want, lse, size = reference(q.double(), k64, v64, [cap], 2)
+    most = torch.exp(torch.stack([(q[0, :, h].double() @ k64[0, :, 0].T).amax(-1) for h in range(2)], -1)[None] / math.sqrt(dh) - lse)
+    # a probability is held to 2^-22 of itself, or to half of fp16's last step lifted by 2^7 and 2^12: 2^-25 2^-19 of the row's largest; scores of up to 24 are off by
+    # 2^-21 of that at worst, sums as in the other tests
+    rel = 2 * 24.0 * 2.0 ** -21 + 2.0 ** -20 + 2.0 ** -24 * (cap / 8 + 64) + 2.0 ** -22
+    tol = rel * size + (2.0 ** -44 * most)[..., None] * v64[0].abs().sum(0).sum(0) + want.abs() * 2.0 ** -24
+    got = out.double().cpu().view_as(want)
+    assert ((got - want).abs() <= tol).all(), ((got - want).abs() / tol).max().item()
