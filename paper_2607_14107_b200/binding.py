@@ -541,11 +541,19 @@ def _row_stride(name: str, t: torch.Tensor, dev: int) -> int:
     return stride[0] if rows > 1 else n
 
 
+def _sizes(**sizes):
+    """Sizes that the library takes as 32-bit integers: ctypes would cut larger ones short without a word."""
+    for name, n in sizes.items():
+        if n > 0x7fffffff:
+            _refuse(f"{name} is {n}, more than 2^31 - 1")
+
+
 def fp4_group(fmt: int) -> int:
     return 16 if fmt == FP4_NV else 32
 
 
 def polestar_k_fp4_scale_bytes(rows: int, d: int, fmt: int, layout: int) -> int:
+    _sizes(d=d)
     return int(load().polestar_k_fp4_scale_bytes(rows, d, fmt, layout))
 
 
@@ -560,6 +568,8 @@ def polestar_k_fp4_quantize(x, codes, scales, fmt: int, layout: int = SCALES_ROW
     dev = _device("x", x)
     ld = _row_stride("x", x, dev)
     rows, d = x.shape
+    if (rows | d) >> 31:
+        _sizes(rows=rows, d=d)
     lib = load()
     if d % 32 or scales.numel() != _scale_bytes(rows, d, fmt, layout):
         _refuse(f"scales have {scales.numel()} bytes, which is not what {rows} rows of {d} channels take")
@@ -575,6 +585,8 @@ def polestar_k_fp4_matmul(a_codes, a_scales, b_codes, b_scales, out, fmt: int, a
     if a_codes.dim() != 2 or b_codes.dim() != 2:
         _refuse("codes have to be matrices")
     (M, half), N = a_codes.shape, b_codes.shape[0]
+    if (M | N | half) >> 30:
+        _sizes(M=M, N=N, K=2 * half)
     lib = load()
     size = _scale_bytes
     if half % 32 or a_scales.numel() != size(M, 2 * half, fmt, SCALES_TILED) or b_scales.numel() != size(N, 2 * half, fmt, SCALES_TILED):
@@ -639,6 +651,8 @@ def polestar_k_token_logprobs(logits, target, mask_id, logprob, entropy, top_ids
     dev = _device("logits", logits)
     ld = _row_stride("logits", logits, dev)
     rows, V = logits.shape
+    if (rows | V) >> 31:
+        _sizes(rows=rows, vocab=V)
     if (top_ids is None) != (top_logprobs is None):
         _refuse("top_ids and top_logprobs come together")
     if top_ids is not None and top_ids.dim() != 2:
@@ -647,6 +661,6 @@ def polestar_k_token_logprobs(logits, target, mask_id, logprob, entropy, top_ids
     f32, i32 = torch.float32, torch.int32
     _check(load().polestar_k_token_logprobs(
         logits.data_ptr(), ld, rows, V, _dtype_code(logits), _address("target", target, i32, dev, (rows,), logprob is None),
-        -1 if mask_id is None else mask_id, k, _address("logprob", logprob, f32, dev, (rows,), True),
+        mask_id if mask_id is not None and 0 <= mask_id < V else -1, k, _address("logprob", logprob, f32, dev, (rows,), True),
         _address("entropy", entropy, f32, dev, (rows,), True), _address("top_ids", top_ids, i32, dev, (rows, k), True),
         _address("top_logprobs", top_logprobs, f32, dev, (rows, k), True), _raw_stream(dev)))

@@ -234,3 +234,12 @@ def test_fp32_probabilities_far_below_the_largest(R, dh):
     tol = rel * size + (2.0 ** -44 * most)[..., None] * v64[0].abs().sum(0).sum(0) + want.abs() * 2.0 ** -24
     got = out.double().cpu().view_as(want)
     assert ((got - want).abs() <= tol).all(), ((got - want).abs() / tol).max().item()
+
+
+@pytest.mark.parametrize("mask_id", [2 ** 32 + 3, 3 - 2 ** 32, 2 ** 31, 100, -1])
+def test_mask_token_out_of_range_leaves_nothing_out(mask_id):
+    x = torch.randn((2, 100), generator=torch.Generator().manual_seed(1))
+    x[:, 3] = 9.0
+    ids, tops = torch.empty((2, 1), dtype=torch.int32, device="cuda"), torch.empty((2, 1), device="cuda")
+    Bd.polestar_k_token_logprobs(x.cuda(), None, mask_id, None, None, ids, tops)
+    assert (ids == 3).all()

@@ -123,3 +123,14 @@ def test_binding_refuses_what_the_library_cannot_see():
         with pytest.raises(Bd.PolestarError) as e:
             call()
         assert e.value.code == Bd.E_INVAL
+
+
+def test_binding_refuses_sizes_beyond_32_bits():
+    # ctypes cuts integers to 32 bits without a word: 2^32 + 64 channels would become 64
+    Bd._sizes(rows=0, d=2 ** 31 - 1)
+    for n in (2 ** 31, 2 ** 32, 2 ** 32 + 64):
+        with pytest.raises(Bd.PolestarError) as e:
+            Bd._sizes(rows=1, d=n)
+        assert e.value.code == Bd.E_INVAL
+        with pytest.raises(Bd.PolestarError):
+            Bd.polestar_k_fp4_scale_bytes(1, n, Bd.FP4_NV, Bd.SCALES_ROWS)
