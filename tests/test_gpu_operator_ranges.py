@@ -243,3 +243,49 @@ def test_mask_token_out_of_range_leaves_nothing_out(mask_id):
     ids, tops = torch.empty((2, 1), dtype=torch.int32, device="cuda"), torch.empty((2, 1), device="cuda")
     Bd.polestar_k_token_logprobs(x.cuda(), None, mask_id, None, None, ids, tops)
     assert (ids == 3).all()
+
+
+@pytest.mark.parametrize("kernel", [1, 2])
+@pytest.mark.parametrize("b,R,cap,nh,nkv,lens", [
+    (1, 300, 2, 2, 1, None), (2, 65, 3, 4, 2, [3, 2]), (1, 200, 7, 1, 1, None), (2, 40, 130, 2, 2, [130, 129]), (3, 16, 700, 4, 1, [700, 257, 5]), (1, 600, 40, 1, 1, None),
+])
+def test_bf16_rows_hold_probabilities_to_11_bits(monkeypatch, kernel, b, R, cap, nh, nkv, lens):
+    # few keys whose values nearly cancel show a probability's rounding, which the outputs' own hides elsewhere
+    force(monkeypatch, kernel)
+    g = torch.Generator().manual_seed(21)
+    k, v = torch.randn((b, cap, nkv, 128), generator=g), torch.randn((b, cap, nkv, 128), generator=g)
+    (kc, ks, k64), (vc, vs, v64) = cache_of(k, v, 0.02, 0.005)
+    q = (torch.randn((b, R, nh, 128), generator=g) * 0.5).bfloat16()
+    out, _ = run(q.flatten(2).cuda(), kc, ks, vc, vs, 0.02, 0.005, lens)
+    n = lens or [cap] * b
+    want, _, size = reference(q.double(), k64, v64, n, nh)
+    # scores as in the other tests: 2^-21 sum |q k| / sqrt(dh) at worst; a probability is off by twice that, by 2^-20 of the exponential and by fp16's half step
+    # 2^-11; sums of `cap` terms in instructions of 16 add 2^-23 (truncated) each; then the output's rounding
+    s_err = torch.zeros((b, R, nh), dtype=torch.float64)
+    for i in range(b):
+        for h in range(nh):
+            s_err[i, :, h] = (q[i, :, h].double().abs() @ k64[i, :n[i], h // (nh // nkv)].abs().T).amax(-1) / math.sqrt(128) * 2.0 ** -21
+    rel = 2 * s_err + 2.0 ** -20 + 2.0 ** -11 + 2.0 ** -23 * (cap / 16 + 8)
+    tol = rel[..., None] * size + want.abs() * 2.0 ** -8
+    got = out.double().cpu().view_as(want)
+    assert ((got - want).abs() <= tol).all(), ((got - want).abs() / tol).max().item()
+
+
+@pytest.mark.parametrize("dh", [64, 128])
+def test_fp32_rows_over_many_keys_keep_their_last_places(dh):
+    # values of one sign and probabilities spread over 20000 keys that no CTAs share out: every warp adds 312 times to its sums, a third of them each.  Rounded to nearest,
+    # the additions' errors (2^-24 of the running sum at most, 2^-25.8 on average in square) have no direction: 3 2^-24 sqrt(312 / 3) 2^-1.8 = 9 2^-24 would be
+    # three of their standard deviations for one output, and their mean square over all outputs is near 3 2^-24.  Probabilities add 2^-22 (their two terms; the
+    # exponential's 2^-22 weighs on sums and values alike), scores 2^-22 here.  Together below 2e-6; sums truncated at every step lose 7e-6 of
+    # themselves (312 additions, each a half of the running sum's last place on average).
+    cap, R, nh = 20000, 260, 28
+    g = torch.Generator().manual_seed(22)
+    k, v = torch.randn((1, cap, 4, dh), generator=g), torch.rand((1, cap, 4, dh), generator=g) + 0.5
+    (kc, ks, k64), (vc, vs, v64) = cache_of(k, v, 0.02, 0.005)
+    q = torch.randn((1, R, nh, dh), generator=g) * 0.05
+    out, lse = run(q.flatten(2).cuda(), kc, ks, vc, vs, 0.02, 0.005, None)
+    rows = torch.tensor([0, 7, 16, 100, 259])
+    want, want_lse, _ = reference(q[:, rows].double(), k64, v64, [cap], nh)
+    got = out.double().cpu().view(1, R, nh, dh)[:, rows]
+    assert ((got - want).norm() / want.norm()).item() <= 2e-6
+    assert (lse.double().cpu()[:, rows] - want_lse).abs().max().item() <= 2e-6 * 10.0
