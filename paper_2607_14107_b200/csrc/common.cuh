@@ -62,7 +62,7 @@ __device__ __forceinline__ uint32_t cluster_rank() {
 // ---- optional kernel timeline (POLESTAR_TRACE builds only) ----------------------------------
 // In a library built with -DPOLESTAR_TRACE, block 0 of every kernel records (kernel id, nanosecond time) once
 // its dependencies are resolved; consecutive stamps give each kernel's real cost inside the pipeline.  The
-// default build compiles none of this.
+// default build compiles none of this.  (Kernels of the decoding path only, polestar.cu: the operators next to it write no stamps.)
 #ifdef POLESTAR_TRACE
 static __device__ long long* g_trace_buf = nullptr;   // [0] = next slot, then pairs (id, time)
 __device__ __forceinline__ void trace_stamp(int id, int thread = 0) {

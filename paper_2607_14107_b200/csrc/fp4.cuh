@@ -193,7 +193,8 @@ struct QuantArgs {
 // Piece i of the call is piece i % ppr of row i / ppr.  A block takes PER x THREADS consecutive ones, all loads of a thread in flight at once.
 template <typename T, int FMT, int PER>
 __global__ void __launch_bounds__(THREADS) quantize_kernel(const __grid_constant__ QuantArgs a) {
-    KERNEL_PROLOGUE(20);   // fp4 quantize_kernel
+    pdl_trigger();
+    pdl_wait();
     constexpr int N = Piece<T>::N, G = group(FMT);
     const int ppr = a.d / N, groups = a.d / G, g4 = (groups + 3) >> 2;
     const Factor t = make_factor<FMT>(a.t);
@@ -267,7 +268,8 @@ constexpr int APPEND_MAX_ROWS = 256;             // rows of a block
 // position a later row lists again: the last one listed stays, whole.
 template <typename T>
 __global__ void __launch_bounds__(THREADS) kv_append_kernel(const __grid_constant__ AppendArgs a) {
-    KERNEL_PROLOGUE(21);   // fp4 kv_append_kernel
+    pdl_trigger();
+    pdl_wait();
     constexpr int N = Piece<T>::N;
     __shared__ int pos[APPEND_MAX_ROWS];
     const int which = blockIdx.z;

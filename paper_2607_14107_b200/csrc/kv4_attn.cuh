@@ -149,7 +149,8 @@ __device__ __forceinline__ uint32_t transpose8x8(uint32_t a) {
 // 2^-25 is lost: entries of q beside much larger ones, and probabilities below 2^-32 of the largest, 65536 of which weigh 2^-16.)
 template <typename T, int DH, int NB>
 __global__ void __launch_bounds__(THREADS) kv4_attn_warp_kernel(const __grid_constant__ Args a) {
-    KERNEL_PROLOGUE(23);   // kv4_attn_warp_kernel
+    pdl_trigger();
+    pdl_wait();
     constexpr int TERMS = sizeof(T) == 4 ? 2 : 1, KS = DH / 16, MT = DH / 16, ROWS = 8 * NB;
     using St = Stage<DH>;
     extern __shared__ uint8_t smem_raw[];
@@ -464,7 +465,8 @@ __global__ void __launch_bounds__(THREADS) kv4_attn_warp_kernel(const __grid_con
 // (statistics, weights, parts, sums): 2.5 - 3 us behind the attention kernel.
 template <typename T, int DH>
 __global__ void __launch_bounds__(JOIN_THREADS) kv4_attn_join_kernel(const __grid_constant__ Args a) {
-    KERNEL_PROLOGUE(24);   // kv4_attn_join_kernel
+    pdl_trigger();
+    pdl_wait();
     constexpr int PER = DH / 32, JW = JOIN_THREADS / 32;
     __shared__ float wgt[MAX_SPLIT], sum[JW][DH];
     __shared__ float red[2][JW];

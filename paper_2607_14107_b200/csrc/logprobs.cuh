@@ -134,7 +134,8 @@ struct Run {
 
 template <typename T>
 __global__ void __launch_bounds__(MAX_THREADS) token_logprobs_kernel(Args a) {
-    KERNEL_PROLOGUE(22);   // token_logprobs_kernel
+    pdl_trigger();
+    pdl_wait();
     constexpr int N = In<T>::N;
     __shared__ float4 parts[MAX_CL * (MAX_THREADS / 32)];
     __shared__ unsigned long long tops[MAX_CL * MAX_K];
