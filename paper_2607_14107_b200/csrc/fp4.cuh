@@ -183,7 +183,7 @@ __device__ __forceinline__ void store_codes(uint8_t* p, const uint32_t (&c)[2]) 
 
 struct QuantArgs {
     const void* x; long long ld_x;       // rows, elements between them
-    void* deq; long long ld_deq;         // stored values (null: not wanted)
+    void* deq;                           // stored values, dense rows (null: not wanted)
     uint8_t* codes; uint8_t* scales;
     const float* t;
     long long rows;
@@ -225,7 +225,7 @@ __global__ void __launch_bounds__(THREADS) quantize_kernel(const __grid_constant
         if (row[i] < 0) continue;
         store_codes(a.codes + row[i] * (a.d >> 1) + c[i] * (N / 2), codes);
         if (a.deq) {
-            uint4* to = reinterpret_cast<uint4*>((T*)a.deq + row[i] * a.ld_deq) + 2 * c[i];
+            uint4* to = reinterpret_cast<uint4*>((T*)a.deq + row[i] * a.d) + 2 * c[i];
             to[0] = stored.w[0];
             to[1] = stored.w[1];
         }

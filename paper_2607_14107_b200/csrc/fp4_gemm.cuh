@@ -412,7 +412,7 @@ gemm_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
         const int quarter = warp & 3, half = (warp - 4) >> 2;
         const uint32_t taddr = tmem + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(half * 128);
         constexpr int PER = 128 / sizeof(OUT), BOXES = 128 / PER;        // columns of a box, boxes of this warp's 128 columns
-        const uint32_t box0 = smem_base + PR_STAGES * STAGE + (uint32_t)(warp - 4) * PR_BOX;
+        const uint32_t box = smem_base + PR_STAGES * STAGE + (uint32_t)(warp - 4) * PR_BOX;
         bool ok = true;
         int n = 0;
         for (int id = pair; id < tiles; id += pairs, ++n) {
@@ -439,41 +439,38 @@ gemm_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
             }
             const int m0 = (tm * 2 + rank) * 128 + quarter * 32, n0 = tn * PR_TILE + half * 128;
             const float nan = __uint_as_float(0x7fc00000u);      // a bounded wait gave up: NaN, not a partial sum
-            {
 #pragma unroll
-                for (int x = 0; x < BOXES; ++x) {
-                    if (m0 >= g.M || n0 + x * PER >= g.N) break;             // (the same for all lanes)
-                    const uint32_t box = box0;
-                    if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");      // the store before has read the box
+            for (int x = 0; x < BOXES; ++x) {
+                if (m0 >= g.M || n0 + x * PER >= g.N) break;             // (the same for all lanes)
+                if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");      // the store before has read the box
+                __syncwarp();
+#pragma unroll
+                for (int c = 0; c < 8; ++c) {                            // sixteen bytes of the lane's row
+                    uint32_t w[4];
+                    constexpr int E = 16 / sizeof(OUT);
+                    float f[E];
+#pragma unroll
+                    for (int i = 0; i < E; ++i) { const int col = x * PER + c * E + i; f[i] = ok ? __uint_as_float(v[col >> 4][col & 15]) * last : nan; }
+                    pack16(w, f);
+                    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(box + (uint32_t)lane * 128u + (uint32_t)((c ^ (lane & 7)) << 4)), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]) : "memory");
+                }
+                if (g.box_out) {
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                     __syncwarp();
-#pragma unroll
-                    for (int c = 0; c < 8; ++c) {                            // sixteen bytes of the lane's row
-                        uint32_t w[4];
-                        constexpr int E = 16 / sizeof(OUT);
-                        float f[E];
-#pragma unroll
-                        for (int i = 0; i < E; ++i) { const int col = x * PER + c * E + i; f[i] = ok ? __uint_as_float(v[col >> 4][col & 15]) * last : nan; }
-                        pack16(w, f);
-                        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(box + (uint32_t)lane * 128u + (uint32_t)((c ^ (lane & 7)) << 4)), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]) : "memory");
+                    if (lane == 0) {
+                        asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%2, %3}], [%1];" ::"l"(&map_out), "r"(box), "r"(n0 + x * PER), "r"(m0) : "memory");
+                        asm volatile("cp.async.bulk.commit_group;" ::: "memory");
                     }
-                    if (g.box_out) {
-                        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                        __syncwarp();
-                        if (lane == 0) {
-                            asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%2, %3}], [%1];" ::"l"(&map_out), "r"(box), "r"(n0 + x * PER), "r"(m0) : "memory");
-                            asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+                } else {
+                    __syncwarp();
+                    const uint8_t* sm = smem + (box - smem_base);
+                    const int rows = min(32, g.M - m0), cols = min(PER, g.N - n0 - x * PER);
+                    OUT* dst = (OUT*)g.out + (long long)m0 * g.ld + n0 + x * PER;
+                    for (int r = 0; r < rows; ++r, dst += g.ld)
+                        for (int c = lane; c < cols; c += 32) {
+                            const int byte = c * (int)sizeof(OUT);
+                            dst[c] = *reinterpret_cast<const OUT*>(sm + r * 128 + (((byte >> 4) ^ (r & 7)) << 4) + (byte & 15));
                         }
-                    } else {
-                        __syncwarp();
-                        const uint8_t* sm = smem + (box - smem_base);
-                        const int rows = min(32, g.M - m0), cols = min(PER, g.N - n0 - x * PER);
-                        OUT* dst = (OUT*)g.out + (long long)m0 * g.ld + n0 + x * PER;
-                        for (int r = 0; r < rows; ++r, dst += g.ld)
-                            for (int c = lane; c < cols; c += 32) {
-                                const int byte = c * (int)sizeof(OUT);
-                                dst[c] = *reinterpret_cast<const OUT*>(sm + r * 128 + (((byte >> 4) ^ (r & 7)) << 4) + (byte & 15));
-                            }
-                    }
                 }
             }
             __syncwarp();

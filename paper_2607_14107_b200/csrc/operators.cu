@@ -108,7 +108,7 @@ extern "C" int polestar_k_fp4_quantize(const void* x, int64_t ld_x, int32_t rows
     int rc = device_info(&di);
     if (rc) return rc;
     fp4::QuantArgs a;
-    a.x = x; a.ld_x = ld_x; a.deq = deq; a.ld_deq = d; a.codes = codes; a.scales = scales; a.t = tensor_scale;
+    a.x = x; a.ld_x = ld_x; a.deq = deq; a.codes = codes; a.scales = scales; a.t = tensor_scale;
     a.rows = rows; a.d = d; a.layout = scale_layout;
     cudaStream_t st = (cudaStream_t)stream;
     const bool nv = format == POLESTAR_FP4_NV;
