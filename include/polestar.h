@@ -421,7 +421,7 @@ int polestar_k_fp4_quantize(const void *x_dev, int64_t ld_x, int32_t rows, int32
  *   a_codes_dev [M][K/2], b_codes_dev [N][K/2] (a weight's [out, in]); scales of both in the TILED layout; all 16-byte aligned
  *   a_tensor_scale_dev / b_tensor_scale_dev: the tensors' factors t (NULL: 1)
  *   out_dev [M][N], F32 or BF16, row stride ld_out elements (>= N)
- * K % 64 == 0; any M and N.  Sums are added in an order that depends on the sizes only. */
+ * K % 64 == 0; any M and N; each at most 2^31 - 256.  Sums are added in an order that depends on the sizes only. */
 int polestar_k_fp4_matmul(const uint8_t *a_codes_dev, const uint8_t *a_scales_dev, const uint8_t *b_codes_dev,
                           const uint8_t *b_scales_dev, const float *a_tensor_scale_dev, const float *b_tensor_scale_dev,
                           void *out_dev, int64_t ld_out, int32_t M, int32_t N, int32_t K, int32_t format, int32_t out_dtype,

@@ -228,6 +228,8 @@ extern "C" int polestar_k_fp4_matmul(const uint8_t* a_codes, const uint8_t* a_sc
                                      const float* a_tensor_scale, const float* b_tensor_scale, void* out, int64_t ld_out, int32_t M,
                                      int32_t N, int32_t K, int32_t format, int32_t out_dtype, void* stream) {
     if (M < 0 || N < 0 || K <= 0 || K % 64 || ld_out < N || !fp4_format_ok(format, POLESTAR_SCALES_TILED)) return POLESTAR_E_INVAL;
+    static_assert(fp4::KB <= 256 && fp4::PR_TILE <= 256, "sizes are rounded up to these in 32 bits");
+    if (std::max(M, std::max(N, K)) > INT32_MAX - 255) return POLESTAR_E_INVAL;
     if (out_dtype != POLESTAR_F32 && out_dtype != POLESTAR_BF16) return POLESTAR_E_INVAL;
     if (M == 0 || N == 0) return POLESTAR_OK;    // nothing to compute (the pointers may be null)
     if (!a_codes || !a_scales || !b_codes || !b_scales || !out) return POLESTAR_E_INVAL;

@@ -134,3 +134,9 @@ def test_binding_refuses_sizes_beyond_32_bits():
         assert e.value.code == Bd.E_INVAL
         with pytest.raises(Bd.PolestarError):
             Bd.polestar_k_fp4_scale_bytes(1, n, Bd.FP4_NV, Bd.SCALES_ROWS)
+
+
+@pytest.mark.parametrize("sizes", [dict(M=2 ** 31 - 1), dict(M=2 ** 31 - 255), dict(N=2 ** 31 - 1, ld=2 ** 31), dict(K=2 ** 31 - 64)])
+def test_matmul_refuses_sizes_that_do_not_round_up_in_32_bits(lib, sizes):
+    # tiles are counted in 32 bits: the last size with a whole tile behind it is 2^31 - 256
+    assert matmul(lib, **sizes) == Bd.E_INVAL
