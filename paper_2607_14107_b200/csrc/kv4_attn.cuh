@@ -10,9 +10,9 @@
 // that 8 query rows fill a product.  A warp copies its own keys' codes into a ring of its own (cp.async, no barrier), and they become operand fragments
 // in registers: the order of channels inside a product is free, so a lane takes its fragments of keys from consecutive channels of a row and those of
 // values from one group of channels, and a scale covers all that it multiplies.  One pass with a running maximum that moves only when it has been
-// outgrown by 2^8.  Bound by instructions: about 420 of a warp for 16 keys, keys and values, and 8 rows (unpacking, scaling and transposing more than products),
-// 58 % of the issue slots busy.  One row of 28 heads, 4 K/V heads, eight ragged sequences of up to 32768 keys 32 us, joining included (85 MB: 2.6 TB/s); 32 rows
-// of 32 heads over 512 keys 10.5 us, a latency chain.  fp32 rows take two terms of q and p, twice the products: the same tokens 52 us for 30000 keys.
+// outgrown by 2^8.  About 420 instructions of a warp for 16 keys, keys and values, and 8 rows (unpacking, scaling and transposing more than products), which
+// keep 57 % of the issue slots busy: registers leave 16 warps to an SM, too few to fill the rest.  One row of 28 heads, 4 K/V heads, eight ragged sequences of up to 32768 keys 32 us, joining included (85 MB: 2.6 TB/s); 32 rows
+// of 32 heads over 512 keys 10.5 us, a latency chain.  fp32 rows take two terms of q and p, twice the products: the same tokens 56 us for 30000 keys.
 #pragma once
 #include <cuda_fp16.h>
 

@@ -16,7 +16,8 @@
 // begun with the old maximum before the new one is known (a longer chain); a form with S^T in tensor memory for up to 64 rows (143 us for 58 at 64 rows,
 // 8 x 2048 keys, 32 heads: its code is fetched once per CTA, and that alone takes longer than the products).
 //
-// fp16 on both sides: keys and values are exact in it, q (bf16) is after a power of two per row, and probabilities keep three more bits than in bf16.
+// fp16 on both sides: keys and values are exact in it, q (bf16) is after a power of two per row down to 2^-17 of the row's largest entry (smaller ones are within
+// 2^-25 of that), and probabilities keep three more bits than in bf16.
 // The method of the two streams and the lagging maximum is that of attn_flash.cuh (published; named there).  Every mbarrier wait is bounded.
 #pragma once
 #include "kv4_attn.cuh"

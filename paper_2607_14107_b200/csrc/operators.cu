@@ -339,7 +339,8 @@ static Kv4Tc kv4_tc_plan(long long batch, long long R, int cap, int n_heads, int
 // tiles.  The warp-level one's time as measured: 1.0 us for 16 rows x 128 keys on an SM, or, three CTAs per SM at a time, 1.4 us of latency for 128 keys of a
 // part while the CTAs have an SM for two of theirs, 3.2 us once they share them (2.4 in long parts), all of it times 0.75 for 8 rows, and 5 us and the joining.  us, warp-level / tensor-core:
 // 7 rows a K/V head, eight ragged sequences of up to 32768 keys 36 / 112; 32 heads, 32 rows, 512 keys 12.9 / 12.7, 8 x 2048 keys 78 / 59; 64 rows, 2048 keys 33 / 19, 8 x 2048
-// 121 / 60; 63 rows x 4 heads, 2048 keys 14.5 / 17.3, 8 x 2048 32 / 20; 896 rows, 65536 keys x 4 heads 814 / 155.
+// 121 / 60; 63 rows x 4 heads, 2048 keys 14.5 / 17.3, 8 x 2048 32 / 20; 896 rows, 65536 keys x 4 heads 814 / 155.  (Next to the border it can be a tenth off: 63 rows x 4
+// heads over 2 x 2048 keys take 15.8 / 17.4, and it picks the second.)
 static bool kv4_use_tc(int dtype, int head_dim, const Kv4Warp& w, const Kv4Tc& t, long long batch, long long R, int cap, int n_heads, int n_kv) {
     if (dtype != POLESTAR_BF16 || head_dim != kv4::TC_DH) return false;
     const int forced = read_switch(g_kv4_kernel);

@@ -289,3 +289,17 @@ def test_fp32_rows_over_many_keys_keep_their_last_places(dh):
     got = out.double().cpu().view(1, R, nh, dh)[:, rows]
     assert ((got - want).norm() / want.norm()).item() <= 2e-6
     assert (lse.double().cpu()[:, rows] - want_lse).abs().max().item() <= 2e-6 * 10.0
+
+
+@pytest.mark.parametrize("kernel,dtype,dh", [(1, "bf16", 128), (2, "bf16", 128), (0, "f32", 128), (0, "bf16", 64)])
+def test_a_score_above_fp32_makes_its_row_nan(monkeypatch, kernel, dtype, dh):
+    force(monkeypatch, kernel)
+    cap, R, tk = 300, 3, 1e7
+    k, v = torch.zeros((1, cap, 1, dh)), torch.ones((1, cap, 1, dh))
+    k[0, 200] = 1e10
+    (kc, ks, _), (vc, vs, _) = cache_of(k, v, tk, 0.01)
+    q = torch.full((1, R, dh), 1e-12)
+    q[0, 1] = 1e30
+    out, lse = run(q.to(DT[dtype]).cuda(), kc, ks, vc, vs, tk, 0.01, [cap])
+    assert torch.isnan(out[0, 1]).all() and torch.isnan(lse[0, 1]).all()
+    assert torch.isfinite(out[0, ::2]).all() and torch.isfinite(lse[0, ::2]).all()
